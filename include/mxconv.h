@@ -650,6 +650,139 @@ int mxconv_quantize_sum_sr(int fmt, int n, int c, int h, int w, int nterms, cons
                            int fn, const void* z, void* codes, uint8_t* scales, float* vals, uint64_t seed,
                            void* stream);
 
+/* ------------------------------------------------------------------ linear layers */
+/* The three products of a linear layer on MX matrices, with the bias, the
+ * activation and the residual in their epilogues.  An MX matrix of R rows and
+ * C columns is the MX tensor of role MXC_WEIGHT and shape (R, C, 1, 1): the
+ * square 32 x 32 blocks serve both directions it is contracted in, so X, W and
+ * dZ are each quantized once (mxconv_quantize, layout MXC_NCHW, of the
+ * row-major matrix; any R and C).  With R a multiple of 32 the tensor of role
+ * MXC_ACT has the same bytes.
+ *   X [rows][ins], W [outs][ins], Z = X W^T + bias [rows][outs], dZ [rows][outs].
+ * Formats: `fmt` as for the convolutions (one, or MXC_PAIR of the call's two
+ * operands in its order; the same pairs).  Products are exact and summed in
+ * fp32, everything in the epilogue is fp32, and a result is rounded once, to
+ * `dtype` (fp32, or bf16 to nearest even).  Full-precision matrices are
+ * row-major with unit column stride and the given row stride in elements (at
+ * least the number of columns, any remainder); pointers are 16-byte aligned.
+ * rows >= 1; outs and ins at most MXC_LINEAR_MAX_DIM.
+ *
+ * Forward:  Y = fn(Z) + residual.
+ *   bias      NULL, or device fp32 [outs].
+ *   residual  NULL, or device `dtype` rows x outs, row stride ldr; it may be Y
+ *             itself (same pointer and stride).
+ *   z         NULL, or device `dtype` rows x outs, row stride ldz: receives Z,
+ *             rounded; fn is applied to the unrounded Z.
+ * Input gradient:  dX = fn'(z) . (dZ W) + residual, rows x ins -- with z the
+ * pre-activation whose activation is this layer's X, the dZ of the layer
+ * before; with the gradient that reached X past this layer as the residual.
+ *   z         device `dtype` rows x ins, row stride ldz; may be NULL for
+ *             MXC_FN_NONE.
+ * Weight gradient:  dW = dZ^T X, fp32 [outs][ins] contiguous; db = the sum of
+ * dZ's rows, fp32 [outs], or NULL.
+ *   workspace  device, >= mxconv_linear_workspace_bytes(op, lin) bytes (may be
+ *              NULL when that is 0): partial sums of a product whose
+ *              contraction is split over workgroups, added in a fixed order.
+ * fn: MXC_FN_NONE, MXC_FN_RELU or MXC_FN_SILU without flags.
+ * Errors: NULL, ARG (enum, sizes, strides), SHAPE (a matrix too large),
+ * ALIGN, WORKSPACE, HIP. */
+#define MXC_LINEAR_MAX_DIM (1 << 20)
+typedef enum { MXC_LINEAR_FWD = 0, MXC_LINEAR_DGRAD = 1, MXC_LINEAR_WGRAD = 2 } mxc_linear_op;
+typedef struct mxc_linear {
+    int32_t rows, outs, ins;
+} mxc_linear;
+size_t mxconv_linear_workspace_bytes(int op, const mxc_linear* lin);
+int mxconv_linear_fwd(const mxc_linear* lin, int fmt,
+                      const void* w_codes, const uint8_t* w_scales,
+                      const void* x_codes, const uint8_t* x_scales,
+                      const float* bias, int fn, const void* residual, int64_t ldr,
+                      void* y, int64_t ldy, void* z, int64_t ldz, int dtype,
+                      void* workspace, size_t ws_bytes, void* stream);
+int mxconv_linear_dgrad(const mxc_linear* lin, int fmt,
+                        const void* w_codes, const uint8_t* w_scales,
+                        const void* dz_codes, const uint8_t* dz_scales,
+                        int fn, const void* z, int64_t ldz, const void* residual, int64_t ldr,
+                        void* dx, int64_t ldx, int dtype,
+                        void* workspace, size_t ws_bytes, void* stream);
+int mxconv_linear_wgrad(const mxc_linear* lin, int fmt,
+                        const void* dz_codes, const uint8_t* dz_scales,
+                        const void* x_codes, const uint8_t* x_scales,
+                        float* dw, float* db,
+                        void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ residual norms */
+/* A residual block's update with the norm behind the block (w_post), its gate
+ * and scale, and the norm in front of the next block (w_pre), in one pass:
+ *   H = X + scale * gate . N(Y; w_post),   U = N(H; w_pre),
+ *   N(v; w) = w . v / sqrt(mean(v^2) + eps) over a row of d values.
+ * All arithmetic is fp32; H and U are rounded once, and U is formed from the
+ * unrounded H.  Row-major matrices of `dtype` (fp32 or bf16), unit column
+ * stride and a row stride in elements (>= d).
+ *   w_post  NULL (N(Y) is then Y itself), or device fp32 [d];
+ *   gate    NULL (1), or device fp32 [gates][d]: row r has gate r / (rows /
+ *           gates); gates divides rows (one gate for all rows: gates = 1);
+ *   w_pre   NULL (no U), or device fp32 [d];
+ *   h, u    written; h may be x itself (same pointer and stride).
+ * Backward, from the gradients dH of H and dU of U, with H and Y as the
+ * forward pass wrote and read them (the statistics are formed again):
+ *   t = dU . w_pre, hh = H r(H):  dX = dH + r(H) (t - hh mean(t . hh)),
+ *   b = scale * gate . dX,  yh = Y r(Y):  dY = r(Y) (b . w_post - yh mean(b . w_post . yh))
+ *   (dY = b without w_post), and fp32, written:
+ *   dw_pre [d] = sum of dU . hh,  dw_post [d] = sum of b . yh,
+ *   dgate [gates][d] = sum over a gate's rows of scale * dX . N(Y; w_post).
+ *   du, h and dw_pre are needed with w_pre, dw_post with w_post, dgate with
+ *   gate.  dx may be dh itself, dy may be y itself.
+ *   workspace  device, >= mxconv_norm_workspace_bytes(...) bytes (may be NULL
+ *              when that is 0): partial column sums, added in a fixed order.
+ * d at most MXC_NORM_MAX_DIM; rows >= 1; eps >= 0 and finite.
+ * Errors: NULL, ARG (enum, sizes, strides, eps), SHAPE (d, or gates that do
+ * not divide rows), ALIGN, WORKSPACE, HIP. */
+#define MXC_NORM_MAX_DIM 8192
+typedef struct mxc_norm {
+    int64_t rows, gates;
+    int32_t d, dtype;
+    float scale, eps;
+    const float* w_post;
+    const float* gate;
+    const float* w_pre;
+} mxc_norm;
+int mxconv_norm_fwd(const mxc_norm* nm, const void* x, int64_t ldx, const void* y, int64_t ldy,
+                    void* h, int64_t ldh, void* u, int64_t ldu, void* stream);
+size_t mxconv_norm_workspace_bytes(const mxc_norm* nm);
+int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void* du, int64_t lddu,
+                    const void* h, int64_t ldh, const void* y, int64_t ldy,
+                    void* dx, int64_t lddx, void* dy, int64_t lddy,
+                    float* dw_pre, float* dw_post, float* dgate,
+                    void* workspace, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------ gradient clipping */
+/* The Euclidean norm of all elements of `count` tensors (a step's weight
+ * gradients) and the tensors scaled to at most max_norm:
+ *   norm = sqrt(sum g^2),  dst = g * min(1, max_norm / (norm + 1e-6)).
+ * The squares are summed in fp64 in a fixed order; the factor is rounded to
+ * fp32, the product is one fp32 operation, rounded once for bf16.  A NaN norm
+ * makes the factor NaN, an infinite one makes it 0.  Tensors are contiguous,
+ * of n >= 0 elements, fp32 or bf16 each.
+ *   dst        every tensor's output (its src: in place), or NULL in all of
+ *              them: only the norm is formed.  Outputs must not overlap each
+ *              other, or a src other than their own.
+ *   max_norm   >= 0 (infinity: never scaled).
+ *   norm       NULL, or device fp32 [1], written (0 for no elements).
+ *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes.
+ * The factor is read on the device: no synchronization.  count >= 0; a launch
+ * takes 96 tensors, more take several.
+ * Errors: NULL, ARG, ALIGN, WORKSPACE, HIP. */
+typedef struct mxc_gtensor {
+    const void* src;
+    void* dst;
+    int64_t n;
+    int32_t dtype;
+} mxc_gtensor;
+#define MXC_CLIP_MAX 65536
+size_t mxconv_grad_clip_workspace_bytes(void);
+int mxconv_grad_clip(int count, const mxc_gtensor* tensors, double max_norm, float* norm,
+                     void* workspace, size_t ws_bytes, void* stream);
+
 /* Human-readable text for a return code (static storage). */
 const char* mxconv_strerror(int code);
 

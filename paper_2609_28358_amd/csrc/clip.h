@@ -1,0 +1,14 @@
+// clip.h -- limits of the gradient-norm kernels (clip.hip), shared with the
+// host-side checks of the C ABI.
+#pragma once
+#include "mx_internal.h"
+
+namespace mxc {
+
+constexpr int CLIP_TENSORS = 96;       // descriptors of a launch (kernel arguments)
+constexpr int CLIP_PARTS = 2048;       // partial sums of all launches
+
+int launch_grad_clip(int count, const mxc_gtensor* t, bool scale, double max_norm, float* norm, void* ws,
+                     hipStream_t s);
+
+}  // namespace mxc

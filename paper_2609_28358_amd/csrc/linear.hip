@@ -1,0 +1,106 @@
+// linear.hip -- the plan of a linear product (tile shape, split of the
+// contraction), its launch, and the kernel that joins split partial sums.
+#include "linear_kern.h"
+
+namespace mxc {
+namespace {
+
+struct LinPlan {
+    int tile, ra, rb, kb;         // tile shape, in 32-blocks; contraction blocks of a stage
+    int ta, tb, nst, nsplit, sps;
+    long long ldw;                // row length of the partial sums
+};
+
+// nra, nrb: 32-blocks along the output's columns and rows; ncb: along the
+// contraction.
+LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
+    LinPlan q;
+    const long long t128 = (long long)((nra + 3) / 4) * ((nrb + 3) / 4);
+    if (op != LIN_WGRAD && nrb == 1) { q.tile = LIN_TILE_ROWS32; q.ra = 1; q.rb = 1; q.kb = 16; }
+    else if (op != LIN_WGRAD && nrb == 2) { q.tile = LIN_TILE_ROWS64; q.ra = 1; q.rb = 2; q.kb = 16; }
+    else if (t128 < 192) { q.tile = LIN_TILE_64; q.ra = 2; q.rb = 2; q.kb = 4; }
+    else { q.tile = LIN_TILE_128; q.ra = 4; q.rb = 4; q.kb = 4; }
+    q.ta = (nra + q.ra - 1) / q.ra;
+    q.tb = (nrb + q.rb - 1) / q.rb;
+    q.nst = (ncb + q.kb - 1) / q.kb;
+    // a grid that leaves CUs idle is split along the contraction, as long as
+    // a split keeps four stages
+    const long long t = (long long)q.ta * q.tb;
+    int n = t < 256 ? (int)std::min<long long>(256 / t, q.nst / 4) : 1;
+    if (n < 1) n = 1;
+    q.sps = (q.nst + n - 1) / n;
+    q.nsplit = (q.nst + q.sps - 1) / q.sps;
+    q.ldw = (long long)nra * 32;
+    return q;
+}
+
+// out[r][c .. c + 3] = epilogue(sum over the splits, in order); the weight
+// gradient's column sums likewise.
+template <int OP>
+__global__ __launch_bounds__(256) void lin_join_kernel(const LinEpi e, const float* __restrict__ part, int nsplit,
+                                                       long long ldw, long long quads, const float* __restrict__ sums,
+                                                       float* __restrict__ colsum) {
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i < quads) {
+        const int per = (e.ncols + 3) / 4;
+        const int r = (int)(i / per), c = (int)(i - (long long)r * per) * 4;
+        const float* p = part + (long long)r * ldw + c;
+        const long long step = (long long)e.nrows * ldw;
+        float4 v = *(const float4*)p;
+        for (int k = 1; k < nsplit; k++) {
+            const float4 u = *(const float4*)(p + k * step);
+            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+        }
+        lin_epilogue4<OP>(e, r, c, v);
+    }
+    if (OP == LIN_WGRAD && colsum && i < e.nrows) {
+        float v = sums[i];
+        for (int k = 1; k < nsplit; k++) v += sums[(long long)k * e.nrows + i];
+        colsum[i] = v;
+    }
+}
+
+int lin_blocks(int n) { return (n + 31) / 32; }
+
+}  // namespace
+
+size_t linear_workspace(int op, int nrows, int ncols, int ncon) {
+    const LinPlan q = lin_plan(op, lin_blocks(ncols), lin_blocks(nrows), lin_blocks(ncon));
+    if (q.nsplit == 1) return 0;
+    return (size_t)q.nsplit * ((size_t)nrows * q.ldw + (op == LIN_WGRAD ? nrows : 0)) * sizeof(float);
+}
+
+int launch_linear(int op, int fa, int fb, const LinMat& a, const LinMat& b, int ncon, const LinEpi& e, float* colsum,
+                  void* ws, hipStream_t s) {
+    const int nra = lin_blocks(e.ncols), nrb = lin_blocks(e.nrows), ncb = lin_blocks(ncon);
+    const LinPlan q = lin_plan(op, nra, nrb, ncb);
+    const long long tiles = (long long)q.ta * q.tb * q.nsplit;
+    if (tiles > (1 << 22)) return MXC_ERR_SHAPE;
+    LinArgs p;
+    // blocks are stored [row block][column block] of the matrix: along the
+    // product's rows where those are the matrix's rows, else along its columns
+    const bool ta = op == LIN_FWD, tb = op != LIN_WGRAD;
+    p.a = {a.codes, a.scales, nra, ncb, ta ? ncb : 1, ta ? 1 : nra};
+    p.b = {b.codes, b.scales, nrb, ncb, tb ? ncb : 1, tb ? 1 : nrb};
+    p.e = e;
+    p.ta = q.ta; p.tb = q.tb; p.nsplit = q.nsplit; p.sps = q.sps;
+    p.ldw = q.ldw;
+    float* const sums = (float*)ws + (size_t)q.nsplit * e.nrows * q.ldw;
+    p.part = q.nsplit > 1 ? (float*)ws : nullptr;
+    p.colsum = colsum && q.nsplit > 1 ? sums : colsum;
+    int rc;
+    if (fa == MXC_E4M3) rc = launch_linear_e4m3(op, p, q.tile, s);
+    else if (fa == MXC_E2M1 && fb == MXC_E2M1) rc = launch_linear_e2m1(op, p, q.tile, s);
+    else rc = launch_linear_fp6(op, fa, fb, p, q.tile, s);
+    if (rc || q.nsplit == 1) return rc;
+    const long long quads = (long long)e.nrows * ((e.ncols + 3) / 4);
+    const long long nthr = std::max<long long>(quads, colsum ? e.nrows : 0);
+    const unsigned grid = (unsigned)((nthr + 255) / 256);
+    if (op == LIN_FWD) lin_join_kernel<LIN_FWD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads, sums, nullptr);
+    else if (op == LIN_DGRAD)
+        lin_join_kernel<LIN_DGRAD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads, sums, nullptr);
+    else lin_join_kernel<LIN_WGRAD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads, sums, colsum);
+    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_HIP;
+}
+
+}  // namespace mxc

@@ -1,0 +1,519 @@
+// linear_kern.h -- the products of a linear layer on MX matrices: the kernel
+// template and its launch, instantiated per format pair in linear_*.hip.
+// Included by .hip files only.
+//
+// An MX matrix of R rows and C columns is an array [ceil(R/32)][ceil(C/32)] of
+// 32 x 32 blocks of codes, each block [column][row] (row fastest), with one
+// E8M0 scale a block.  The square blocks serve both directions, so the three
+// products of a layer (Y = X W^T, dX = dZ W, dW = dZ^T X) read the same stored
+// blocks of X [rows][ins], W [outs][ins] and dZ [rows][outs]:
+//   operand    product rows   contraction   stored order
+//   fwd    W   outs           ins           row fastest: transposed reads
+//   fwd    X   rows           ins           transposed reads
+//   dgrad  W   ins            outs          contraction fastest: direct reads
+//   dgrad  dZ  rows           outs          transposed reads
+//   wgrad  X   ins            rows          direct reads
+//   wgrad  dZ  outs           rows          direct reads
+// The operand whose rows are the output's columns is the MFMA's first (A), so
+// a lane's accumulator holds four consecutive output columns of one output
+// row and the epilogue moves vectors.
+#pragma once
+#include <atomic>
+
+#include "mx_internal.h"
+
+namespace mxc {
+
+// One operand: blocks along the product's rows and along the contraction, and
+// the block strides of both (in blocks).
+struct LinOp {
+    const uint8_t* codes;
+    const uint8_t* scales;
+    int nrb, ncb;
+    int srow, scon;
+};
+
+// The epilogue: out[r][c] for output row r < nrows, column c < ncols.
+//   fwd    z = v + bias[c]; pre[r][c] = z; out = fn(z) + res[r][c]
+//   dgrad  out = v fn'(z[r][c]) + res[r][c]
+// pre doubles as dgrad's z.  vec: every pointer and stride allows vectors of
+// four columns, and ncols is a multiple of four.
+struct LinEpi {
+    void* out;
+    const float* bias;
+    const void* res;
+    void* pre;
+    long long ldo, ldr, ldp;
+    int fn, bf16, vec;
+    int nrows, ncols;
+};
+
+// A stored matrix.
+struct LinMat {
+    const uint8_t* codes;
+    const uint8_t* scales;
+};
+
+struct LinArgs {
+    LinOp a, b;
+    LinEpi e;
+    float* part;          // split contraction: partial sums [split][nrows][ldw], else NULL
+    long long ldw;
+    float* colsum;        // weight gradient: db (or its partial sums [split][nrows]), or NULL
+    int ta, tb;           // tiles along A's and B's rows
+    int nsplit, sps;      // splits, stages of each
+};
+
+enum { LIN_FWD = 0, LIN_DGRAD = 1, LIN_WGRAD = 2 };
+
+// Tile shapes: blocks a wave holds (MB x NB), waves along A's rows, along B's
+// rows and along the contraction, 32-blocks of the contraction a wave takes
+// from a stage, and stages in the ring.
+template <int MB_, int NB_, int WM_, int WN_, int WK_, int KS_, int NBUF_> struct LinTile {
+    static constexpr int MB = MB_, NB = NB_, WM = WM_, WN = WN_, WK = WK_, KS = KS_, NBUF = NBUF_;
+    static constexpr int RA = MB * WM, RB = NB * WN, KB = KS * WK, W = WM * WN * WK;
+};
+
+// LDS bytes of one block, blocks a 64-lane copy of 16 bytes a lane moves, and
+// the source bytes a lane advances (FP6: 12 of a half row, in 16-byte slots)
+template <int F> struct LinBlk {
+    static constexpr int SRC = 32 * 32 * fmt_bits(F) / 8;
+    static constexpr int LDS = fmt_bits(F) == 4 ? 512 : 1024;
+    static constexpr int BPI = fmt_bits(F) == 4 ? 2 : 1;
+    static constexpr int STEP = fmt_bits(F) == 6 ? 12 : 16;
+};
+
+template <int FA, int FB, class T> struct LinLds {
+    static constexpr int ABYTES = T::RA * T::KB * LinBlk<FA>::LDS;
+    static constexpr int BBYTES = T::RB * T::KB * LinBlk<FB>::LDS;
+    static constexpr int NSI = ((T::RA + T::RB) * T::KB + 63) / 64;          // scale copies of a stage
+    static constexpr int STAGE = ABYTES + BBYTES + NSI * 256;
+    static constexpr int RED = T::WK > 1 ? T::W * T::MB * T::NB * 4096 : 0;  // joining the waves of the contraction
+    static constexpr int BYTES = T::NBUF * STAGE > RED ? T::NBUF * STAGE : RED;
+};
+
+// tile shapes a launch is asked for: outputs of at most 32 or 64 rows (the
+// contraction is shared by a workgroup's waves), 64 x 64, 128 x 128
+enum { LIN_TILE_ROWS32 = 0, LIN_TILE_ROWS64 = 1, LIN_TILE_64 = 2, LIN_TILE_128 = 3 };
+
+// linear.hip: workspace bytes and launch of one product (nrows x ncols
+// outputs over ncon, formats and matrices in the order A, B)
+size_t linear_workspace(int op, int nrows, int ncols, int ncon);
+int launch_linear(int op, int fa, int fb, const LinMat& a, const LinMat& b, int ncon, const LinEpi& e, float* colsum,
+                  void* ws, hipStream_t s);
+// linear_*.hip, by format
+int launch_linear_e4m3(int op, const LinArgs& a, int tile, hipStream_t s);
+int launch_linear_e2m1(int op, const LinArgs& a, int tile, hipStream_t s);
+int launch_linear_fp6(int op, int fa, int fb, const LinArgs& a, int tile, hipStream_t s);
+
+}  // namespace mxc
+
+#if defined(__HIPCC__)
+namespace mxc {
+
+static __device__ __attribute__((aligned(16))) uint8_t g_lin_zero[1024];
+
+// A 16-byte copy a lane to LDS from a uniform base and a lane offset: the
+// base advances on the scalar unit.
+__device__ __forceinline__ void dma16_base(const uint8_t* base, uint32_t off, uint32_t lds) {
+    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(lds) : "memory");
+}
+
+// ---------------------------------------------------------------- epilogue
+template <int OP>
+__device__ __forceinline__ float lin_value(const LinEpi& e, float v, float b, float z, float r) {
+    if constexpr (OP == LIN_FWD) {
+        v += b;
+        return (e.fn == MXC_FN_NONE ? v : e.fn == MXC_FN_RELU ? fn_apply_c<MXC_FN_RELU>(v) : fn_apply_c<MXC_FN_SILU>(v)) + r;
+    } else if constexpr (OP == LIN_DGRAD) {
+        return (e.fn == MXC_FN_NONE ? v : v * fn_grad(e.fn, z)) + r;
+    } else {
+        return v;
+    }
+}
+
+__device__ __forceinline__ float4 lin_load4(const void* p, long long i, int bf16) {
+    return bf16 ? bf16_unpack4(*(const uint2*)((const uint16_t*)p + i)) : *(const float4*)((const float*)p + i);
+}
+__device__ __forceinline__ void lin_store4(void* p, long long i, int bf16, float4 v) {
+    if (bf16) *(uint2*)((uint16_t*)p + i) = bf16_pack4(v.x, v.y, v.z, v.w);
+    else *(float4*)((float*)p + i) = v;
+}
+__device__ __forceinline__ float lin_load1(const void* p, long long i, int bf16) {
+    return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16) : ((const float*)p)[i];
+}
+__device__ __forceinline__ void lin_store1(void* p, long long i, int bf16, float v) {
+    if (bf16) ((uint16_t*)p)[i] = (uint16_t)bf16_bits(v);
+    else ((float*)p)[i] = v;
+}
+
+// Four consecutive columns c .. c + 3 of output row r (r < nrows; columns past
+// ncols are dropped).  All arithmetic is fp32, rounded once where it is
+// stored; the activation is applied to the unrounded pre-activation.
+template <int OP>
+__device__ __forceinline__ void lin_epilogue4(const LinEpi& e, int r, int c, float4 v) {
+    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (e.vec) {
+        if (c >= e.ncols) return;
+        float4 b = zero, z = zero, s = zero;
+        if (OP == LIN_FWD && e.bias) b = *(const float4*)(e.bias + c);
+        if (OP == LIN_DGRAD && e.fn != MXC_FN_NONE) z = lin_load4(e.pre, r * e.ldp + c, e.bf16);
+        if (OP != LIN_WGRAD && e.res) s = lin_load4(e.res, r * e.ldr + c, e.bf16);
+        if (OP == LIN_FWD && e.pre)
+            lin_store4(e.pre, r * e.ldp + c, e.bf16, make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w));
+        lin_store4(e.out, r * e.ldo + c, e.bf16,
+                   make_float4(lin_value<OP>(e, v.x, b.x, z.x, s.x), lin_value<OP>(e, v.y, b.y, z.y, s.y),
+                               lin_value<OP>(e, v.z, b.z, z.z, s.z), lin_value<OP>(e, v.w, b.w, z.w, s.w)));
+    } else {
+        const float a[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            if (c + q >= e.ncols) return;
+            const float b = OP == LIN_FWD && e.bias ? e.bias[c + q] : 0.0f;
+            const float z = OP == LIN_DGRAD && e.fn != MXC_FN_NONE ? lin_load1(e.pre, r * e.ldp + c + q, e.bf16) : 0.0f;
+            const float s = OP != LIN_WGRAD && e.res ? lin_load1(e.res, r * e.ldr + c + q, e.bf16) : 0.0f;
+            if (OP == LIN_FWD && e.pre) lin_store1(e.pre, r * e.ldp + c + q, e.bf16, a[q] + b);
+            lin_store1(e.out, r * e.ldo + c + q, e.bf16, lin_value<OP>(e, a[q], b, z, s));
+        }
+    }
+}
+
+// ---------------------------------------------------------------- fragments
+// The fragment (see mfma_mx) of a 32-row block for two contraction blocks at
+// p and p + next (LDS).  TR: rows fastest in the block, read transposed;
+// otherwise the contraction is fastest and a lane's row is contiguous.
+template <int F, bool TR>
+__device__ __forceinline__ v8i lin_frag(const uint8_t* p, int next, int lane) {
+    v8i o;
+    const int h = lane >> 5, i16 = lane & 15, cg = (lane >> 4) & 1;
+    if constexpr (TR && F == MXC_E4M3) {
+        const uint8_t* q = p + (16 * h + (i16 >> 1)) * 32 + 16 * cg + 8 * (i16 & 1);
+#pragma unroll
+        for (int kb = 0; kb < 2; kb++)
+#pragma unroll
+            for (int hf = 0; hf < 2; hf++) {
+                const v2i v = lds_tr8(q + kb * next + hf * 256);
+                o[4 * kb + 2 * hf] = v[0];
+                o[4 * kb + 2 * hf + 1] = v[1];
+            }
+    } else if constexpr (TR && F == MXC_E2M1) {
+        const uint8_t* q = p + h * next + i16 * 16 + 8 * cg;
+#pragma unroll
+        for (int hf = 0; hf < 2; hf++) {
+            const v2i v = lds_tr4(q + hf * 256);
+            o[2 * hf] = v[0];
+            o[2 * hf + 1] = v[1];
+        }
+        o[4] = o[5] = o[6] = o[7] = 0;
+    } else if constexpr (TR) {
+        const uint8_t* q = p + h * next + i16 * 32 + 16 * cg;
+        const v3i lo = lds_tr6(q), hi = lds_tr6(q + 512);
+        o[0] = lo[0]; o[1] = lo[1]; o[2] = lo[2];
+        o[3] = hi[0]; o[4] = hi[1]; o[5] = hi[2];
+        o[6] = o[7] = 0;
+    } else if constexpr (F == MXC_E4M3) {
+        const uint8_t* q = p + (lane & 31) * 32 + 16 * h;
+        const v4i u = *(const v4i*)q, w = *(const v4i*)(q + next);
+#pragma unroll
+        for (int e = 0; e < 4; e++) { o[e] = u[e]; o[4 + e] = w[e]; }
+    } else if constexpr (F == MXC_E2M1) {
+        const v4i u = *(const v4i*)(p + h * next + (lane & 31) * 16);
+#pragma unroll
+        for (int e = 0; e < 4; e++) { o[e] = u[e]; o[4 + e] = 0; }
+    } else {
+        const uint8_t* q = p + h * next + (lane & 31) * 32;
+        const v3i lo = *(const v3i*)q, hi = *(const v3i*)(q + 16);
+        o[0] = lo[0]; o[1] = lo[1]; o[2] = lo[2];
+        o[3] = hi[0]; o[4] = hi[1]; o[5] = hi[2];
+        o[6] = o[7] = 0;
+    }
+    return o;
+}
+
+// Wait until the oldest of `later` + 1 stages of PER copies each is complete.
+template <int PER>
+__device__ __forceinline__ void lin_wait(int later) {
+    static_assert(2 * PER <= 63, "two stages in flight must fit the vmcnt counter");
+    if (later <= 0) vm_wait<0>();
+    else if (later == 1) vm_wait<PER>();
+    else vm_wait<2 * PER>();
+}
+
+// ---------------------------------------------------------------- the product
+// A workgroup computes RA x RB blocks of 32 x 32 outputs.  A stage holds KB
+// contraction blocks of both operands, copied to LDS by global -> LDS loads
+// into a ring of NBUF stages, so NBUF - 2 stages are in flight while one is
+// multiplied; one barrier a stage publishes it and frees the stage before.
+// Row blocks past the end read the last one (their products are not stored);
+// contraction blocks past the end read zero codes and scales.
+template <int FA, int FB, int OP, class T>
+__global__ __launch_bounds__(T::W * 64) void linear_kernel(const LinArgs p) {
+    constexpr int MB = T::MB, NB = T::NB, WM = T::WM, WN = T::WN, WK = T::WK, KS = T::KS, NBUF = T::NBUF;
+    constexpr int RA = T::RA, RB = T::RB, KB = T::KB, W = T::W;
+    constexpr bool TA = OP == LIN_FWD, TB = OP != LIN_WGRAD;      // transposed reads
+    constexpr bool X8 = FA == MXC_E4M3;
+    using BA = LinBlk<FA>;
+    using BB = LinBlk<FB>;
+    using L = LinLds<FA, FB, T>;
+    constexpr int NA = RA * KB / BA::BPI, NSL = NA + RB * KB / BB::BPI;   // 1 KB copies of a stage
+    constexpr int NQ = NSL / W, NSQ = (L::NSI + W - 1) / W, PER = NQ + NSQ;
+    static_assert(NSL % W == 0 && RA * KB % BA::BPI == 0 && RB * KB % BB::BPI == 0 && KS % 2 == 0, "whole copies");
+    static_assert(NBUF >= 2 && NBUF <= 4, "ring");
+    static_assert(MB * NB <= 16, "accumulators");
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // workgroups are dealt round-robin to the 8 XCDs: each XCD takes a
+    // contiguous run of tiles, so tiles that share an operand share its L2
+    const int ntiles = p.ta * p.tb * p.nsplit;
+    const int per = (ntiles + 7) / 8;
+    const int lin = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    if (lin >= ntiles) return;
+    // runs of up to 8 tiles along B inside a column of A's tiles
+    const int split = lin / (p.ta * p.tb), t2 = lin - split * (p.ta * p.tb);
+    const int band = t2 / (8 * p.ta), in_band = t2 - band * 8 * p.ta;
+    const int bw = min(8, p.tb - band * 8);
+    const int ia = in_band / bw, ib = band * 8 + (in_band - ia * bw);
+    const int ra0 = ia * RA, rb0 = ib * RB;
+
+    const int kbeg = split * p.sps * KB;
+    const int kend = min(p.a.ncb, kbeg + p.sps * KB);
+    const int nst = (kend - kbeg + KB - 1) / KB;
+
+    // ---- this lane's part of each copy: block (row block, contraction block)
+    auto blk_of = [&](int q, int& rb, int& kb) {
+        const int slice = q * W + wave;
+        const bool isb = slice >= NA;
+        const int n = isb ? (slice - NA) * BB::BPI + (BB::BPI == 2 ? lane >> 5 : 0)
+                          : slice * BA::BPI + (BA::BPI == 2 ? lane >> 5 : 0);
+        const bool tr = isb ? TB : TA;
+        const int R = isb ? RB : RA;
+        rb = tr ? n / KB : n % R;                 // transposed operands: the contraction is contiguous
+        kb = tr ? n % KB : n / R;
+        return isb;
+    };
+    uint32_t off[NQ];
+#pragma unroll
+    for (int q = 0; q < NQ; q++) {
+        int rb, kb;
+        const bool isb = blk_of(q, rb, kb);
+        const LinOp& o = isb ? p.b : p.a;
+        const int r0 = isb ? rb0 : ra0;
+        const uint32_t in = isb ? (uint32_t)(BB::BPI == 2 ? lane & 31 : lane) * BB::STEP
+                                : (uint32_t)(BA::BPI == 2 ? lane & 31 : lane) * BA::STEP;
+        off[q] = (uint32_t)((min(r0 + rb, o.nrb - 1) - r0) * o.srow + kb * o.scon) * (uint32_t)(isb ? BB::SRC : BA::SRC) + in;
+    }
+    const uint8_t* abase = p.a.codes + ((size_t)ra0 * p.a.srow + (size_t)kbeg * p.a.scon) * BA::SRC;
+    const uint8_t* bbase = p.b.codes + ((size_t)rb0 * p.b.srow + (size_t)kbeg * p.b.scon) * BB::SRC;
+    const size_t astep = (size_t)KB * p.a.scon * BA::SRC, bstep = (size_t)KB * p.b.scon * BB::SRC;
+    // scale entry e of a stage: [contraction block][row block] of A, then of B
+    const uint8_t* sp[NSQ];
+    uint32_t sstep[NSQ];
+    int skb[NSQ];
+#pragma unroll
+    for (int q = 0; q < NSQ; q++) {
+        const int e = ((q * W + wave) % L::NSI) * 64 + lane;
+        const bool isb = e >= RA * KB;
+        const int n = isb ? e - RA * KB : e, R = isb ? RB : RA;
+        const LinOp& o = isb ? p.b : p.a;
+        const int r0 = isb ? rb0 : ra0;
+        const int kb = n / R, row = min(r0 + n % R, o.nrb - 1);
+        const bool ok = e < (RA + RB) * KB;
+        skb[q] = ok ? kb : 0x40000000;
+        sp[q] = o.scales + (ok ? (size_t)row * o.srow + (size_t)(kbeg + kb) * o.scon : 0);
+        sstep[q] = (uint32_t)(KB * o.scon);
+    }
+
+    int kis = kbeg;                               // first contraction block of the next stage to copy
+    auto issue = [&](int buf) {
+        const uint8_t* lds = smem + buf * L::STAGE;
+        if (kis + KB <= kend) {
+#pragma unroll
+            for (int q = 0; q < NQ; q++) {
+                const int slice = q * W + wave;
+                dma16_base(slice >= NA ? bbase : abase, off[q], lds_addr(lds + slice * 1024));
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < NQ; q++) {
+                const int slice = q * W + wave;
+                int rb, kb;
+                const bool isb = blk_of(q, rb, kb);
+                dma16_async(kis + kb < kend ? (isb ? bbase : abase) + off[q] : g_lin_zero + lane * 16,
+                            lds_addr(lds + slice * 1024));
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < NSQ; q++) {
+            dma1_async(kis + skb[q] < kend ? sp[q] : g_lin_zero,
+                       lds_addr(lds + L::ABYTES + L::BBYTES + ((q * W + wave) % L::NSI) * 256));
+            sp[q] += sstep[q];
+        }
+        abase += astep;
+        bbase += bstep;
+        kis += KB;
+    };
+
+    const int wk = wave / (WM * WN), wmn = wave - wk * (WM * WN), wm = wmn % WM, wn = wmn / WM;
+    v16f acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; i++)
+#pragma unroll
+        for (int j = 0; j < NB; j++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) acc[i][j][e] = 0.0f;
+    // weight gradient: the column sums of dZ are one more row of the product,
+    // with ones; the workgroups of the first tile along A take them
+    const bool sums = OP == LIN_WGRAD && p.colsum != nullptr && ia == 0 && wm == 0;
+    v16f csum[OP == LIN_WGRAD ? NB : 1];
+    if constexpr (OP == LIN_WGRAD) {
+#pragma unroll
+        for (int j = 0; j < NB; j++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) csum[j][e] = 0.0f;
+    }
+
+    for (int j = 0; j < NBUF - 1 && j < nst; j++) issue(j);
+    int buf = 0;
+    for (int st = 0; st < nst; st++) {
+        lin_wait<PER>(min(NBUF - 2, nst - 1 - st));
+        __syncthreads();
+        if (st + NBUF - 1 < nst) issue(buf == 0 ? NBUF - 1 : buf - 1);
+        const uint8_t* A = smem + buf * L::STAGE;
+        const uint8_t* B = A + L::ABYTES;
+        const uint8_t* SC = B + L::BBYTES;
+        buf = buf + 1 == NBUF ? 0 : buf + 1;
+#pragma unroll
+        for (int s = 0; s < KS / 2; s++) {
+            const int k0 = wk * KS + 2 * s;
+            auto blk = [&](bool tr, int R, int lds, int rb) {      // LDS offset of (row block rb, k0)
+                return (tr ? rb * KB + k0 : k0 * R + rb) * lds;
+            };
+            v8i fb[NB];
+            int sb[NB];
+            uint32_t db[X8 ? NB : 1][16];
+#pragma unroll
+            for (int j = 0; j < NB; j++) {
+                const int rb = wn * NB + j;
+                fb[j] = lin_frag<FB, TB>(B + blk(TB, RB, BB::LDS, rb), (TB ? 1 : RB) * BB::LDS, lane);
+                const uint8_t* sc = SC + 4 * (RA * KB + k0 * RB + rb);
+                if constexpr (X8) e4m3_decode32(fb[j], *(const int*)sc, *(const int*)(sc + 4 * RB), db[j]);
+                else sb[j] = *(const int*)(sc + (lane >> 5) * 4 * RB);
+            }
+            if constexpr (OP == LIN_WGRAD) {
+                if (sums) {
+#pragma unroll
+                    for (int j = 0; j < NB; j++) {
+                        if constexpr (X8) {
+                            uint32_t one[16];
+#pragma unroll
+                            for (int e = 0; e < 16; e++) one[e] = 0x3F803F80u;
+                            csum[j] = mfma_x8(one, db[j], csum[j]);
+                        } else {
+                            v8i one;      // E2M1 code 2 is 1.0
+#pragma unroll
+                            for (int e = 0; e < 8; e++) one[e] = e < 4 ? 0x22222222 : 0;
+                            csum[j] = mfma_mx<MXC_E2M1, FB>(one, fb[j], csum[j], 127, sb[j]);
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < MB; i++) {
+                const int ra = wm * MB + i;
+                const v8i fa = lin_frag<FA, TA>(A + blk(TA, RA, BA::LDS, ra), (TA ? 1 : RA) * BA::LDS, lane);
+                const uint8_t* sc = SC + 4 * (k0 * RA + ra);
+                if constexpr (X8) {
+                    uint32_t da[16];
+                    e4m3_decode32(fa, *(const int*)sc, *(const int*)(sc + 4 * RA), da);
+#pragma unroll
+                    for (int j = 0; j < NB; j++) acc[i][j] = mfma_x8(da, db[j], acc[i][j]);
+                } else {
+                    const int sa = *(const int*)(sc + (lane >> 5) * 4 * RA);
+#pragma unroll
+                    for (int j = 0; j < NB; j++) acc[i][j] = mfma_mx<FA, FB>(fa, fb[j], acc[i][j], sa, sb[j]);
+                }
+            }
+        }
+    }
+
+    // ---- write: lane l holds output row l % 32 of B's block and, in quad q,
+    // columns 8 q + 4 (l / 32) .. + 3 of A's block
+    auto put = [&](int r, int c, float4 v) {
+        if (r >= p.e.nrows) return;
+        if (p.part) {
+            if (c < p.ldw) *(float4*)(p.part + ((size_t)split * p.e.nrows + r) * p.ldw + c) = v;
+        } else {
+            lin_epilogue4<OP>(p.e, r, c, v);
+        }
+    };
+    if constexpr (OP == LIN_WGRAD) {
+        if (sums && WK == 1 && lane < 32) {
+#pragma unroll
+            for (int j = 0; j < NB; j++) {
+                const int r = (rb0 + wn * NB + j) * 32 + lane;
+                if (r < p.e.nrows) p.colsum[(size_t)split * p.e.nrows + r] = csum[j][0];
+            }
+        }
+    }
+    if constexpr (WK == 1) {
+#pragma unroll
+        for (int i = 0; i < MB; i++)
+#pragma unroll
+            for (int j = 0; j < NB; j++)
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    put((rb0 + wn * NB + j) * 32 + (lane & 31), (ra0 + wm * MB + i) * 32 + 8 * q + 4 * (lane >> 5),
+                        make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
+    } else {
+        // the waves of one output block add their parts in order, through LDS
+        static_assert(OP != LIN_WGRAD || WK == 1, "column sums are not joined");
+        __syncthreads();                          // every wave is done with the ring
+        float4* red = (float4*)smem;              // [wk][wave of the tile][block][quad][lane]
+        constexpr int BL = MB * NB * 256;         // float4s of a wave
+#pragma unroll
+        for (int i = 0; i < MB; i++)
+#pragma unroll
+            for (int j = 0; j < NB; j++)
+#pragma unroll
+                for (int q = 0; q < 4; q++)
+                    red[(wk * WM * WN + wmn) * BL + (i * NB + j) * 256 + q * 64 + lane] =
+                        make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+        __syncthreads();
+        for (int n = tid; n < WM * WN * BL; n += W * 64) {
+            float4 v = red[n];
+#pragma unroll
+            for (int k = 1; k < WK; k++) {
+                const float4 u = red[k * WM * WN * BL + n];
+                v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+            }
+            const int l = n & 63, q = (n >> 6) & 3, b = (n >> 8) % (MB * NB), w = (n >> 8) / (MB * NB);
+            put((rb0 + (w / WM) * NB + b % NB) * 32 + (l & 31), (ra0 + (w % WM) * MB + b / NB) * 32 + 8 * q + 4 * (l >> 5), v);
+        }
+    }
+}
+
+template <int FA, int FB, int OP, class T>
+int linear_launch(const LinArgs& a, hipStream_t s) {
+    static std::atomic<uint64_t> devs{0};
+    constexpr int lds = LinLds<FA, FB, T>::BYTES;
+    static_assert(lds <= 163840, "LDS of a CU");
+    auto kernel = linear_kernel<FA, FB, OP, T>;
+    if (lds > 65536) {                            // above 64 KB the attribute is raised, once per device
+        int dev = 0;
+        if (hipGetDevice(&dev) != hipSuccess) return MXC_ERR_HIP;
+        const uint64_t bit = dev < 64 ? (uint64_t)1 << dev : 0;
+        if (!bit || !(devs.load(std::memory_order_acquire) & bit)) {
+            if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) != hipSuccess)
+                return MXC_ERR_HIP;
+            devs.fetch_or(bit, std::memory_order_release);
+        }
+    }
+    const long long tiles = (long long)a.ta * a.tb * a.nsplit;
+    kernel<<<(unsigned)((tiles + 7) / 8 * 8), T::W * 64, lds, s>>>(a);
+    return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_HIP;
+}
+
+}  // namespace mxc
+#endif

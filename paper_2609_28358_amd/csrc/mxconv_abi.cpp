@@ -1,9 +1,14 @@
 // mxconv_abi.cpp -- the C ABI of include/mxconv.h: host-side validation,
 // size helpers and dispatch to the gfx950 kernels.  Every argument check runs
 // on the host before anything is enqueued.
+#include <cmath>
+#include <initializer_list>
 #include <mutex>
 
+#include "clip.h"
+#include "linear_kern.h"
 #include "mx_internal.h"
+#include "norm.h"
 
 namespace mxc {
 
@@ -596,6 +601,197 @@ int mxconv_naive_wgrad(const mxc_conv* p, int fmt, const void* gtc, const uint8_
     if (!aligned16(gtc) || !aligned16(gts) || !aligned16(xtc) || !aligned16(xts) || !aligned16(gw))
         return MXC_ERR_ALIGN;
     return launch_naive_wgrad(cv, gtc, gts, xtc, xts, gw, (hipStream_t)stream);
+}
+
+// ---- linear layers
+// The formats of a linear product's operands (in the call's order).
+static int linear_fmts(int fmt, int* f1, int* f2) {
+    if ((fmt & ~0x1F) != 0) return MXC_ERR_ARG;
+    *f1 = *f2 = fmt;
+    if (fmt & 0x10) { *f1 = (fmt >> 2) & 3; *f2 = fmt & 3; }
+    return fmt_ok(*f1) && fmt_ok(*f2) && pair_ok(*f1, *f2) ? MXC_OK : MXC_ERR_ARG;
+}
+
+static int linear_check(const mxc_linear* p) {
+    if (p->rows <= 0 || p->outs <= 0 || p->ins <= 0) return MXC_ERR_ARG;
+    if (p->outs > MXC_LINEAR_MAX_DIM || p->ins > MXC_LINEAR_MAX_DIM) return MXC_ERR_SHAPE;
+    Geom g;     // the stored matrices' own limits
+    int rc;
+    if ((rc = geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->rows, p->ins, 1, 1))) return rc;
+    if ((rc = geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->outs, p->ins, 1, 1))) return rc;
+    return geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->rows, p->outs, 1, 1);
+}
+
+// rows, columns and contraction length of a product's output
+static void linear_dims(int op, const mxc_linear& p, int* nrows, int* ncols, int* ncon) {
+    *nrows = op == MXC_LINEAR_WGRAD ? p.outs : p.rows;
+    *ncols = op == MXC_LINEAR_FWD ? p.outs : p.ins;
+    *ncon = op == MXC_LINEAR_FWD ? p.ins : op == MXC_LINEAR_DGRAD ? p.outs : p.rows;
+}
+
+static bool fn_plain_ok(int fn) { return fn == MXC_FN_NONE || fn == MXC_FN_RELU || fn == MXC_FN_SILU; }
+
+// The launch shared by the three products, after their own argument checks.
+static int linear_run(int op, const mxc_linear& p, int fa, int fb, const LinMat& a, const LinMat& b, LinEpi& e,
+                      float* colsum, void* ws, size_t ws_bytes, void* stream) {
+    int ncon;
+    linear_dims(op, p, &e.nrows, &e.ncols, &ncon);
+    const size_t need = linear_workspace(op, e.nrows, e.ncols, ncon);
+    if (need && (!ws || ws_bytes < need)) return MXC_ERR_WORKSPACE;
+    if (!aligned16(a.codes) || !aligned16(a.scales) || !aligned16(b.codes) || !aligned16(b.scales) ||
+        !aligned16(e.out) || !aligned16(e.res) || !aligned16(e.pre) || !aligned16(e.bias) || !aligned16(colsum) ||
+        (need && !aligned16(ws)))
+        return MXC_ERR_ALIGN;
+    e.vec = e.ncols % 4 == 0 && e.ldo % 4 == 0 && (!e.res || e.ldr % 4 == 0) && (!e.pre || e.ldp % 4 == 0);
+    return launch_linear(op, fa, fb, a, b, ncon, e, colsum, ws, (hipStream_t)stream);
+}
+
+size_t mxconv_linear_workspace_bytes(int op, const mxc_linear* p) {
+    if (!p || op < MXC_LINEAR_FWD || op > MXC_LINEAR_WGRAD || linear_check(p)) return 0;
+    int nrows, ncols, ncon;
+    linear_dims(op, *p, &nrows, &ncols, &ncon);
+    return linear_workspace(op, nrows, ncols, ncon);
+}
+
+int mxconv_linear_fwd(const mxc_linear* p, int fmt, const void* wc, const uint8_t* ws, const void* xc,
+                      const uint8_t* xs, const float* bias, int fn, const void* residual, int64_t ldr, void* y,
+                      int64_t ldy, void* z, int64_t ldz, int dtype, void* workspace, size_t ws_bytes, void* stream) {
+    if (!p || !wc || !ws || !xc || !xs || !y) return MXC_ERR_NULL;
+    int fw, fx, rc;
+    if ((rc = linear_fmts(fmt, &fw, &fx)) || (rc = linear_check(p))) return rc;
+    if (!fn_plain_ok(fn) || (dtype != MXC_F32 && dtype != MXC_BF16)) return MXC_ERR_ARG;
+    if (ldy < p->outs || (residual && ldr < p->outs) || (z && ldz < p->outs)) return MXC_ERR_ARG;
+    if (z == y || (residual == y && ldr != ldy)) return MXC_ERR_ARG;
+    LinEpi e = {y, bias, residual, z, ldy, ldr, ldz, fn, dtype == MXC_BF16, 0, 0, 0};
+    return linear_run(LIN_FWD, *p, fw, fx, {(const uint8_t*)wc, ws}, {(const uint8_t*)xc, xs}, e, nullptr, workspace,
+                      ws_bytes, stream);
+}
+
+int mxconv_linear_dgrad(const mxc_linear* p, int fmt, const void* wc, const uint8_t* ws, const void* gc,
+                        const uint8_t* gs, int fn, const void* z, int64_t ldz, const void* residual, int64_t ldr,
+                        void* dx, int64_t ldx, int dtype, void* workspace, size_t ws_bytes, void* stream) {
+    if (!p || !wc || !ws || !gc || !gs || !dx) return MXC_ERR_NULL;
+    int fw, fg, rc;
+    if ((rc = linear_fmts(fmt, &fw, &fg)) || (rc = linear_check(p))) return rc;
+    if (!fn_plain_ok(fn) || (dtype != MXC_F32 && dtype != MXC_BF16)) return MXC_ERR_ARG;
+    if (fn != MXC_FN_NONE && !z) return MXC_ERR_NULL;
+    if (fn == MXC_FN_NONE) z = nullptr;
+    if (ldx < p->ins || (residual && ldr < p->ins) || (z && ldz < p->ins)) return MXC_ERR_ARG;
+    if ((residual == dx && ldr != ldx) || (z == dx && ldz != ldx)) return MXC_ERR_ARG;
+    LinEpi e = {dx, nullptr, residual, const_cast<void*>(z), ldx, ldr, ldz, fn, dtype == MXC_BF16, 0, 0, 0};
+    return linear_run(LIN_DGRAD, *p, fw, fg, {(const uint8_t*)wc, ws}, {(const uint8_t*)gc, gs}, e, nullptr, workspace,
+                      ws_bytes, stream);
+}
+
+int mxconv_linear_wgrad(const mxc_linear* p, int fmt, const void* gc, const uint8_t* gs, const void* xc,
+                        const uint8_t* xs, float* dw, float* db, void* workspace, size_t ws_bytes, void* stream) {
+    if (!p || !gc || !gs || !xc || !xs || !dw) return MXC_ERR_NULL;
+    int fg, fx, rc;
+    if ((rc = linear_fmts(fmt, &fg, &fx)) || (rc = linear_check(p))) return rc;
+    LinEpi e = {dw, nullptr, nullptr, nullptr, p->ins, 0, 0, MXC_FN_NONE, 0, 0, 0, 0};
+    return linear_run(LIN_WGRAD, *p, fx, fg, {(const uint8_t*)xc, xs}, {(const uint8_t*)gc, gs}, e, db, workspace,
+                      ws_bytes, stream);
+}
+
+// ---- residual norms
+static int norm_check(const mxc_norm* p) {
+    if (p->rows <= 0 || p->d <= 0 || (p->dtype != MXC_F32 && p->dtype != MXC_BF16)) return MXC_ERR_ARG;
+    if (!(p->eps >= 0.0f) || std::isinf(p->eps)) return MXC_ERR_ARG;
+    if (p->gate && p->gates <= 0) return MXC_ERR_ARG;
+    if (p->d > MXC_NORM_MAX_DIM || p->rows > (1ll << 40)) return MXC_ERR_SHAPE;
+    if (p->gate && p->rows % p->gates) return MXC_ERR_SHAPE;
+    return MXC_OK;
+}
+
+static NormArgs norm_args(const mxc_norm& p) {
+    NormArgs a = {};
+    a.w_post = p.w_post; a.w_pre = p.w_pre; a.gate = p.gate;
+    a.rows = p.rows;
+    a.gates = p.gate ? p.gates : 1;
+    a.gate_rows = p.rows / a.gates;
+    a.d = p.d;
+    a.scale = p.scale; a.eps = p.eps; a.inv_d = 1.0f / (float)p.d;
+    return a;
+}
+
+// 16-byte vectors: the row length and every stride in use a multiple of them
+static bool norm_vec(const mxc_norm& p, std::initializer_list<int64_t> strides) {
+    const int v = p.dtype == MXC_BF16 ? 8 : 4;
+    if (p.d % v) return false;
+    for (int64_t s : strides)
+        if (s % v) return false;
+    return true;
+}
+
+int mxconv_norm_fwd(const mxc_norm* p, const void* x, int64_t ldx, const void* y, int64_t ldy, void* h, int64_t ldh,
+                    void* u, int64_t ldu, void* stream) {
+    if (!p || !x || !y || !h || (p->w_pre && !u)) return MXC_ERR_NULL;
+    const int rc = norm_check(p);
+    if (rc) return rc;
+    if (!p->w_pre) { u = nullptr; ldu = p->d; }
+    if (ldx < p->d || ldy < p->d || ldh < p->d || ldu < p->d) return MXC_ERR_ARG;
+    if (u == h || (h == x && ldh != ldx)) return MXC_ERR_ARG;
+    if (!aligned16(x) || !aligned16(y) || !aligned16(h) || !aligned16(u) || !aligned16(p->w_post) ||
+        !aligned16(p->gate) || !aligned16(p->w_pre))
+        return MXC_ERR_ALIGN;
+    NormArgs a = norm_args(*p);
+    a.x = x; a.y = y; a.h = h; a.u = u;
+    a.ldx = ldx; a.ldy = ldy; a.ldh = ldh; a.ldu = ldu;
+    const bool vec = norm_vec(*p, {ldx, ldy, ldh, p->w_pre ? ldu : 0});
+    return launch_norm_fwd(a, p->dtype == MXC_BF16, vec, (hipStream_t)stream);
+}
+
+size_t mxconv_norm_workspace_bytes(const mxc_norm* p) {
+    if (!p || norm_check(p)) return 0;
+    return norm_bwd_workspace(p->rows, p->d, p->gate ? p->gates : 1, p->gate, p->w_post, p->w_pre);
+}
+
+int mxconv_norm_bwd(const mxc_norm* p, const void* dh, int64_t lddh, const void* du, int64_t lddu, const void* h,
+                    int64_t ldh, const void* y, int64_t ldy, void* dx, int64_t lddx, void* dy, int64_t lddy,
+                    float* dw_pre, float* dw_post, float* dgate, void* workspace, size_t ws_bytes, void* stream) {
+    if (!p || !dh || !y || !dx || !dy) return MXC_ERR_NULL;
+    if (p->w_pre && (!du || !h || !dw_pre)) return MXC_ERR_NULL;
+    if ((p->w_post && !dw_post) || (p->gate && !dgate)) return MXC_ERR_NULL;
+    const int rc = norm_check(p);
+    if (rc) return rc;
+    if (!p->w_pre) { du = h = nullptr; lddu = ldh = p->d; }
+    if (lddh < p->d || lddu < p->d || ldh < p->d || ldy < p->d || lddx < p->d || lddy < p->d) return MXC_ERR_ARG;
+    if (dx == dy || (dx == dh && lddx != lddh) || (dy == y && lddy != ldy)) return MXC_ERR_ARG;
+    const size_t need = mxconv_norm_workspace_bytes(p);
+    if (need && (!workspace || ws_bytes < need)) return MXC_ERR_WORKSPACE;
+    if (!aligned16(dh) || !aligned16(du) || !aligned16(h) || !aligned16(y) || !aligned16(dx) || !aligned16(dy) ||
+        !aligned16(p->w_post) || !aligned16(p->gate) || !aligned16(p->w_pre) || !aligned16(dw_pre) ||
+        !aligned16(dw_post) || !aligned16(dgate) || (need && !aligned16(workspace)))
+        return MXC_ERR_ALIGN;
+    NormArgs a = norm_args(*p);
+    a.x = dh; a.y = y; a.h = const_cast<void*>(h); a.u = const_cast<void*>(du);
+    a.dx = dx; a.dy = dy;
+    a.ldx = lddh; a.ldy = ldy; a.ldh = ldh; a.ldu = lddu; a.lddx = lddx; a.lddy = lddy;
+    const bool vec = norm_vec(*p, {lddh, ldy, p->w_pre ? ldh : 0, p->w_pre ? lddu : 0, lddx, lddy});
+    return launch_norm_bwd(a, p->dtype == MXC_BF16, vec, dw_pre, dw_post, dgate, workspace, (hipStream_t)stream);
+}
+
+// ---- gradient clipping
+size_t mxconv_grad_clip_workspace_bytes(void) { return (size_t)CLIP_PARTS * sizeof(double); }
+
+int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* norm, void* workspace, size_t ws_bytes,
+                     void* stream) {
+    if (count < 0 || count > MXC_CLIP_MAX || !(max_norm >= 0.0)) return MXC_ERR_ARG;
+    if ((count > 0 && !t) || !workspace) return MXC_ERR_NULL;
+    if (ws_bytes < mxconv_grad_clip_workspace_bytes()) return MXC_ERR_WORKSPACE;
+    if (!aligned16(workspace) || !aligned16(norm)) return MXC_ERR_ALIGN;
+    int full = -1;                                            // a tensor that is not empty
+    for (int i = 0; i < count; i++) {
+        if (t[i].n < 0 || t[i].n > (1ll << 36) || (t[i].dtype != MXC_F32 && t[i].dtype != MXC_BF16)) return MXC_ERR_ARG;
+        if (!t[i].n) continue;                                // an empty tensor's pointers are not looked at
+        if (full < 0) full = i;
+        if (!t[i].src) return MXC_ERR_NULL;
+        if (!t[i].dst != !t[full].dst) return MXC_ERR_ARG;    // outputs for all tensors or for none
+        if (!aligned16(t[i].src) || !aligned16(t[i].dst)) return MXC_ERR_ALIGN;
+    }
+    const bool scale = full >= 0 && t[full].dst;
+    if (!scale && !norm) return full >= 0 ? MXC_ERR_NULL : MXC_OK;   // nothing to write
+    return launch_grad_clip(count, t, scale, max_norm, norm, workspace, (hipStream_t)stream);
 }
 
 const char* mxconv_strerror(int code) {

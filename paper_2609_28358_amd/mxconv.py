@@ -5,9 +5,11 @@ caller's device, pointers and the current HIP stream are passed through, and
 every step runs in the library's HIP kernels.  A missing library raises; there
 is no fallback path.
 """
+import contextlib
 import ctypes
 import functools
 import os
+from array import array
 from operator import itemgetter
 
 import torch
@@ -49,6 +51,16 @@ CONCAT_MAX = 4
 TERMS_MAX = 4
 
 
+class MxcLinear(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("rows", "outs", "ins")]
+
+
+class MxcNorm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("gates", ctypes.c_int64), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("eps", ctypes.c_float), ("w_post", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("w_pre", ctypes.c_void_p)]
+
+
 class MxcPart(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("ncb", ctypes.c_int32),
                 ("up", ctypes.c_int32)]
@@ -76,7 +88,7 @@ def lib():
                           "`python -m paper_2609_28358_amd.build` (no CPU fallback exists)")
     L = ctypes.CDLL(LIB_PATH)
     P, i32, i64, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
-    CP = ctypes.POINTER(MxcConv)
+    CP, LP, NP = (ctypes.POINTER(t) for t in (MxcConv, MxcLinear, MxcNorm))
     sigs = {
         "mxconv_codes_bytes": (sz, [i32] * 6),
         "mxconv_scales_bytes": (sz, [i32] * 6),
@@ -116,6 +128,15 @@ def lib():
         "mxconv_quantize_sum": (i32, [i32, i32, i32, i32, i32, i32, ctypes.POINTER(MxcTerm), i32, P, P, P, P, P]),
         "mxconv_quantize_sum_sr": (i32, [i32, i32, i32, i32, i32, i32, ctypes.POINTER(MxcTerm), i32, P, P, P, P,
                                          ctypes.c_uint64, P]),
+        "mxconv_linear_workspace_bytes": (sz, [i32, LP]),
+        "mxconv_linear_fwd": (i32, [LP, i32, P, P, P, P, P, i32, P, i64, P, i64, P, i64, i32, P, sz, P]),
+        "mxconv_linear_dgrad": (i32, [LP, i32, P, P, P, P, i32, P, i64, P, i64, P, i64, i32, P, sz, P]),
+        "mxconv_linear_wgrad": (i32, [LP, i32, P, P, P, P, P, P, P, sz, P]),
+        "mxconv_norm_fwd": (i32, [NP, P, i64, P, i64, P, i64, P, i64, P]),
+        "mxconv_norm_workspace_bytes": (sz, [NP]),
+        "mxconv_norm_bwd": (i32, [NP, P, i64, P, i64, P, i64, P, i64, P, i64, P, i64, P, P, P, P, sz, P]),
+        "mxconv_grad_clip_workspace_bytes": (sz, []),
+        "mxconv_grad_clip": (i32, [i32, P, ctypes.c_double, P, P, sz, P]),
         "mxconv_strerror": (ctypes.c_char_p, [i32]),
     }
     for name, (res, args) in sigs.items():
@@ -562,6 +583,257 @@ def quantize_sum(terms, shape, fmt, fn=FN_NONE, z=None, out=None, vals=None, str
     else:
         _check(lib().mxconv_quantize_sum_sr(*args, sr_seed, _stream(stream)), "mxconv_quantize_sum_sr")
     return g
+
+
+# ---------------------------------------------------------------- linear layers, residual norms, clipping
+# These calls check what a pointer cannot say (device, type, strides, sizes),
+# run with the tensors' device current, and allocate on the stream they launch
+# on: a workspace freed at return is reused only by later work of that stream.
+LINEAR_FWD, LINEAR_DGRAD, LINEAR_WGRAD = 0, 1, 2
+_here = contextlib.nullcontext()
+
+
+def _place(device, stream):
+    """The context of a call: the device, and the stream where one is given."""
+    if device.type != "cuda":
+        raise MxconvError(f"tensors must be on a GPU, got {device}")
+    if stream is not None:
+        if stream.device != device:
+            raise MxconvError(f"the stream is on {stream.device}, the tensors on {device}")
+        return torch.cuda.stream(stream)
+    return _here if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _rows_cols(t, what, rows, cols, dtype, device):
+    """The row stride of a row-major full-precision matrix argument."""
+    if t is None:
+        return 0
+    if t.dtype != dtype:
+        raise MxconvError(f"{what} must be {dtype}, got {t.dtype}")
+    if t.shape != (rows, cols):
+        raise MxconvError(f"{what} must be {rows} x {cols}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise MxconvError(f"{what} must be on {device}, got {t.device}")
+    if cols > 1 and t.stride(1) != 1:
+        raise MxconvError(f"{what} must have unit column stride")
+    return t.stride(0) if rows > 1 else cols
+
+
+def _vector(t, what, shape, device):
+    """An fp32 parameter argument."""
+    if t is None:
+        return
+    if t.dtype != torch.float32 or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise MxconvError(f"{what} must be a contiguous fp32 tensor of shape {tuple(shape)} on {device}")
+
+
+def _mx_matrix(q, what):
+    """(rows, columns) of an MX matrix argument: shape (R, C, 1, 1) with 32-row
+    blocks."""
+    r, c, h, w = q.shape
+    if h != 1 or w != 1 or (q.role == ACT and r % 32):
+        raise MxconvError(f"{what} must be an MX matrix: shape (R, C, 1, 1), role WEIGHT (or ACT with R a multiple of 32)")
+    if (q.codes.dtype != torch.uint8 or q.scales.dtype != torch.uint8 or not q.codes.is_contiguous() or
+            not q.scales.is_contiguous() or q.codes.numel() < codes_bytes(WEIGHT, q.fmt, r, c, 1, 1) or
+            q.scales.numel() < scales_bytes(WEIGHT, q.fmt, r, c, 1, 1) or q.scales.device != q.codes.device):
+        raise MxconvError(f"{what}: codes and scales must be contiguous uint8 tensors of the matrix's size on one device")
+    return r, c
+
+
+@functools.lru_cache(maxsize=_CACHED)
+def _linear_of(rows, outs, ins):
+    """The layer's struct (only read by the library) and its workspace sizes."""
+    s = MxcLinear(rows, outs, ins)
+    return s, tuple(lib().mxconv_linear_workspace_bytes(op, ctypes.byref(s)) for op in range(3))
+
+
+def linear_workspace_bytes(op, rows, outs, ins):
+    return _linear_of(rows, outs, ins)[1][op]
+
+
+def _workspace(ws, need, device):
+    """(tensor to keep, pointer, bytes) of a call's workspace."""
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    elif ws.device != device or not ws.is_contiguous():
+        raise MxconvError(f"the workspace must be a contiguous tensor on {device}")
+    return ws, _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0
+
+
+def quantize_matrix(m, fmt, out=None, stream=None):
+    """The MX matrix of a contiguous fp32 or bf16 matrix [R][C], an operand of
+    the linear products in any of its roles: quantize() with role WEIGHT and
+    shape (R, C, 1, 1)."""
+    if m.dim() != 2:
+        raise MxconvError("quantize_matrix needs a matrix")
+    return quantize(m, WEIGHT, fmt, shape=(m.shape[0], m.shape[1], 1, 1), out=out, stream=stream)
+
+
+def linear(w, x, bias=None, fn=FN_NONE, residual=None, dtype=torch.bfloat16, out=None, pre_out=None, workspace=None,
+           stream=None):
+    """Y = fn(X W^T + bias) + residual, [rows][outs] of `dtype`, from the MX
+    matrices W [outs][ins] and X [rows][ins] (mxconv_linear_fwd).  pre_out
+    receives X W^T + bias."""
+    (outs, ins), (rows, k), dev = _mx_matrix(w, "w"), _mx_matrix(x, "x"), x.codes.device
+    if k != ins or w.codes.device != dev:
+        raise MxconvError(f"w is {outs} x {ins} on {w.codes.device}, x {rows} x {k} on {dev}")
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise MxconvError(f"unsupported dtype {dtype}")
+    _vector(bias, "bias", (outs,), dev)
+    ldr = _rows_cols(residual, "residual", rows, outs, dtype, dev)
+    ldz = _rows_cols(pre_out, "pre_out", rows, outs, dtype, dev)
+    s, need = _linear_of(rows, outs, ins)
+    with _place(dev, stream):
+        y = out if out is not None else torch.empty((rows, outs), dtype=dtype, device=dev)
+        ldy = _rows_cols(y, "the output", rows, outs, dtype, dev)
+        ws, wp, wb = _workspace(workspace, need[0], dev)
+        _check(lib().mxconv_linear_fwd(ctypes.byref(s), pair(w.fmt, x.fmt), _ptr(w.codes), _ptr(w.scales), _ptr(x.codes),
+                                       _ptr(x.scales), _ptr(bias), fn, _ptr(residual), ldr, _ptr(y), ldy, _ptr(pre_out),
+                                       ldz, code, wp, wb, _stream(stream)), "mxconv_linear_fwd")
+    return y
+
+
+def linear_dgrad(w, dz, fn=FN_NONE, z=None, add=None, dtype=torch.bfloat16, out=None, workspace=None, stream=None):
+    """dX = fn'(z) . (dZ W) + add, [rows][ins] of `dtype`, from the MX matrices
+    W [outs][ins] and dZ [rows][outs] (mxconv_linear_dgrad)."""
+    (outs, ins), (rows, n), dev = _mx_matrix(w, "w"), _mx_matrix(dz, "dz"), dz.codes.device
+    if n != outs or w.codes.device != dev:
+        raise MxconvError(f"w is {outs} x {ins} on {w.codes.device}, dz {rows} x {n} on {dev}")
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise MxconvError(f"unsupported dtype {dtype}")
+    ldz = _rows_cols(z, "z", rows, ins, dtype, dev)
+    lda = _rows_cols(add, "add", rows, ins, dtype, dev)
+    s, need = _linear_of(rows, outs, ins)
+    with _place(dev, stream):
+        dx = out if out is not None else torch.empty((rows, ins), dtype=dtype, device=dev)
+        ldx = _rows_cols(dx, "the output", rows, ins, dtype, dev)
+        ws, wp, wb = _workspace(workspace, need[1], dev)
+        _check(lib().mxconv_linear_dgrad(ctypes.byref(s), pair(w.fmt, dz.fmt), _ptr(w.codes), _ptr(w.scales),
+                                         _ptr(dz.codes), _ptr(dz.scales), fn, _ptr(z), ldz, _ptr(add), lda, _ptr(dx), ldx,
+                                         code, wp, wb, _stream(stream)), "mxconv_linear_dgrad")
+    return dx
+
+
+def linear_wgrad(dz, x, bias=True, out=None, bias_out=None, workspace=None, stream=None):
+    """(dW, db): dZ^T X, fp32 [outs][ins], and the column sums of dZ, fp32
+    [outs] (None with bias=False), from the MX matrices dZ [rows][outs] and
+    X [rows][ins] (mxconv_linear_wgrad)."""
+    (rows, outs), (r2, ins), dev = _mx_matrix(dz, "dz"), _mx_matrix(x, "x"), x.codes.device
+    if r2 != rows or dz.codes.device != dev:
+        raise MxconvError(f"dz is {rows} x {outs} on {dz.codes.device}, x {r2} x {ins} on {dev}")
+    s, need = _linear_of(rows, outs, ins)
+    with _place(dev, stream):
+        dw = out if out is not None else torch.empty((outs, ins), dtype=torch.float32, device=dev)
+        _vector(dw, "the output", (outs, ins), dev)
+        db = bias_out if bias_out is not None or not bias else torch.empty((outs,), dtype=torch.float32, device=dev)
+        _vector(db, "bias_out", (outs,), dev)
+        ws, wp, wb = _workspace(workspace, need[2], dev)
+        _check(lib().mxconv_linear_wgrad(ctypes.byref(s), pair(dz.fmt, x.fmt), _ptr(dz.codes), _ptr(dz.scales),
+                                         _ptr(x.codes), _ptr(x.scales), _ptr(dw), _ptr(db), wp, wb, _stream(stream)),
+               "mxconv_linear_wgrad")
+    return dw, db
+
+
+def _norm_struct(y, w_post, gate, scale, w_pre, eps):
+    if y.dim() != 2 or y.dtype not in _DTYPES:
+        raise MxconvError("the residual norms need fp32 or bf16 matrices")
+    rows, d = y.shape
+    if gate is not None and gate.dim() == 1:
+        gate = gate[None]
+    if gate is not None and (gate.dim() != 2 or gate.shape[0] == 0 or rows % gate.shape[0]):
+        raise MxconvError(f"gate must be [d] or [gates][d] with gates dividing the {rows} rows, got {tuple(gate.shape)}")
+    gates = gate.shape[0] if gate is not None else 1
+    for t, what, shape in ((w_post, "w_post", (d,)), (w_pre, "w_pre", (d,)), (gate, "gate", (gates, d))):
+        _vector(t, what, shape, y.device)
+    return MxcNorm(rows, gates, d, _DTYPES[y.dtype], scale, eps, _ptr(w_post), _ptr(gate), _ptr(w_pre)), gates
+
+
+def norm_residual(x, y, w_post=None, gate=None, scale=1.0, w_pre=None, eps=1e-6, h_out=None, u_out=None, stream=None):
+    """(H, U): H = x + scale * gate . N(y; w_post) and U = N(H; w_pre), N(v; w)
+    = w . v / sqrt(mean(v^2) + eps) by rows (mxconv_norm_fwd).  x, y: [rows][d],
+    fp32 or bf16; w_post, w_pre: fp32 [d] or None (N(y) is y; no U); gate: fp32
+    [d], [gates][d] (each for rows / gates consecutive rows) or None."""
+    s, _ = _norm_struct(y, w_post, gate, scale, w_pre, eps)
+    (rows, d), dt, dev = y.shape, y.dtype, y.device
+    ldx, ldy = _rows_cols(x, "x", rows, d, dt, dev), _rows_cols(y, "y", rows, d, dt, dev)
+    with _place(dev, stream):
+        h = h_out if h_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
+        u = None
+        if w_pre is not None:
+            u = u_out if u_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
+        ldh, ldu = _rows_cols(h, "h_out", rows, d, dt, dev), _rows_cols(u, "u_out", rows, d, dt, dev)
+        _check(lib().mxconv_norm_fwd(ctypes.byref(s), _ptr(x), ldx, _ptr(y), ldy, _ptr(h), ldh, _ptr(u), ldu,
+                                     _stream(stream)), "mxconv_norm_fwd")
+    return h, u
+
+
+def norm_residual_backward(dh, du, h, y, w_post=None, gate=None, scale=1.0, w_pre=None, eps=1e-6, dx_out=None, dy_out=None,
+                           workspace=None, stream=None):
+    """(dX, dY, dw_pre, dw_post, dgate) of norm_residual from the gradients dh
+    of H and du of U, with H and y of the forward pass (mxconv_norm_bwd).  du
+    and h may be None without w_pre; the gradients of absent parameters are
+    None; dgate is [gates][d]."""
+    s, gates = _norm_struct(y, w_post, gate, scale, w_pre, eps)
+    (rows, d), dt, dev = y.shape, y.dtype, y.device
+    if w_pre is None:
+        du = h = None
+    elif du is None or h is None:
+        raise MxconvError("the backward pass of w_pre needs du and h")
+    lds = [_rows_cols(t, n, rows, d, dt, dev) for t, n in ((dh, "dh"), (du, "du"), (h, "h"), (y, "y"))]
+    with _place(dev, stream):
+        dx = dx_out if dx_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
+        dy = dy_out if dy_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
+        lddx, lddy = _rows_cols(dx, "dx_out", rows, d, dt, dev), _rows_cols(dy, "dy_out", rows, d, dt, dev)
+        dw_pre, dw_post, dgate = (torch.empty(sh, dtype=torch.float32, device=dev) if t is not None else None
+                                  for t, sh in ((w_pre, (d,)), (w_post, (d,)), (gate, (gates, d))))
+        ws, wp, wb = _workspace(workspace, lib().mxconv_norm_workspace_bytes(ctypes.byref(s)), dev)
+        _check(lib().mxconv_norm_bwd(ctypes.byref(s), _ptr(dh), lds[0], _ptr(du), lds[1], _ptr(h), lds[2], _ptr(y), lds[3],
+                                     _ptr(dx), lddx, _ptr(dy), lddy, _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), wp, wb,
+                                     _stream(stream)), "mxconv_norm_bwd")
+    return dx, dy, dw_pre, dw_post, dgate
+
+
+def _clip(tensors, outs, max_norm, norm_out, workspace, stream):
+    if not tensors:
+        raise MxconvError("no tensors")
+    dev = tensors[0].device
+    desc = array("q")
+    for t, o in zip(tensors, outs if outs is not None else tensors):
+        code = _DTYPES.get(t.dtype)
+        if code is None or t.device != dev or not t.is_contiguous():
+            raise MxconvError(f"gradients must be contiguous fp32 or bf16 tensors on {dev}")
+        n = t.numel()
+        if o is not t and (o.dtype != t.dtype or o.numel() != n or o.device != dev or not o.is_contiguous()):
+            raise MxconvError("an output must be contiguous and have its gradient's size, type and device")
+        desc.extend((t.data_ptr(), o.data_ptr() if outs is not None else 0, n, code))
+    written = [p for p, n in zip(desc[1::4], desc[2::4]) if p and n]
+    if len(set(written)) != len(written):
+        raise MxconvError("a tensor is written twice")
+    with _place(dev, stream):
+        norm = norm_out if norm_out is not None else torch.empty((), dtype=torch.float32, device=dev)
+        if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != dev:
+            raise MxconvError(f"norm_out must be one fp32 element on {dev}")
+        ws, wp, wb = _workspace(workspace, lib().mxconv_grad_clip_workspace_bytes(), dev)
+        _check(lib().mxconv_grad_clip(len(tensors), desc.buffer_info()[0], max_norm, _ptr(norm), wp, wb, _stream(stream)),
+               "mxconv_grad_clip")
+    return norm
+
+
+def grad_norm(tensors, norm_out=None, workspace=None, stream=None):
+    """The Euclidean norm of all elements of the tensors, an fp32 device scalar."""
+    return _clip(tensors, None, float("inf"), norm_out, workspace, stream)
+
+
+def grad_clip(tensors, max_norm, out=None, norm_out=None, workspace=None, stream=None):
+    """Scale the tensors (contiguous fp32 or bf16) by min(1, max_norm / (norm +
+    1e-6)), norm = their Euclidean norm together, into `out` (tensors of the
+    same sizes and types; None: in place).  Returns the norm before scaling, an
+    fp32 device scalar; nothing is synchronized (mxconv_grad_clip)."""
+    if out is not None and len(out) != len(tensors):
+        raise MxconvError(f"{len(out)} outputs for {len(tensors)} tensors")
+    return _clip(tensors, tensors if out is None else out, max_norm, norm_out, workspace, stream)
 
 
 # ---------------------------------------------------------------- naive comparator
