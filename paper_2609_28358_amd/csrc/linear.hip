@@ -6,40 +6,39 @@ namespace mxc {
 namespace {
 
 struct LinPlan {
-    int tile, ra, rb, kb;         // tile shape, in 32-blocks; contraction blocks of a stage
-    int ta, tb, nst, nsplit, sps;
+    int tile, ra, rb;             // tile shape, in 32-blocks
+    int ta, tb, nsplit, span;     // tiles; splits of the contraction, blocks of each
     long long ldw;                // row length of the partial sums
 };
 
 // nra, nrb: 32-blocks along the output's columns and rows; ncb: along the
-// contraction.
+// contraction.  The formats play no part, so neither do they in the workspace.
 LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
     LinPlan q;
-    const long long t128 = (long long)((nra + 3) / 4) * ((nrb + 3) / 4);
-    if (op != LIN_WGRAD && nrb == 1) { q.tile = LIN_TILE_ROWS32; q.ra = 1; q.rb = 1; q.kb = 16; }
-    else if (op != LIN_WGRAD && nrb == 2) { q.tile = LIN_TILE_ROWS64; q.ra = 1; q.rb = 2; q.kb = 16; }
-    else if (t128 < 192) { q.tile = LIN_TILE_64; q.ra = 2; q.rb = 2; q.kb = 4; }
-    else { q.tile = LIN_TILE_128; q.ra = 4; q.rb = 4; q.kb = 4; }
+    auto tiles = [&](int a, int b) { return (long long)((nra + a - 1) / a) * ((nrb + b - 1) / b); };
+    if (op != LIN_WGRAD && nrb == 1) { q.tile = LIN_TILE_ROWS32; q.ra = 1; q.rb = 1; }
+    else if (op != LIN_WGRAD && nrb == 2) { q.tile = LIN_TILE_ROWS64; q.ra = 1; q.rb = 2; }
+    else if (tiles(8, 4) >= 512) { q.tile = LIN_TILE_256; q.ra = 8; q.rb = 4; }
+    else if (tiles(4, 4) >= 256) { q.tile = LIN_TILE_128; q.ra = 4; q.rb = 4; }
+    else { q.tile = LIN_TILE_64; q.ra = 2; q.rb = 2; }
     q.ta = (nra + q.ra - 1) / q.ra;
     q.tb = (nrb + q.rb - 1) / q.rb;
-    q.nst = (ncb + q.kb - 1) / q.kb;
-    // a grid that leaves CUs idle is split along the contraction, as long as
-    // a split keeps four stages
+    // a grid that leaves CUs idle is split along the contraction, in units of
+    // 16 blocks (a whole number of any shape's stages), two of them a split at
+    // least, four where a stage is a whole unit
     const long long t = (long long)q.ta * q.tb;
-    int n = t < 256 ? (int)std::min<long long>(256 / t, q.nst / 4) : 1;
-    if (n < 1) n = 1;
-    q.sps = (q.nst + n - 1) / n;
-    q.nsplit = (q.nst + q.sps - 1) / q.sps;
+    const int units = (ncb + 15) / 16;
+    const int n = t < 256 ? std::max(1, (int)std::min<long long>(256 / t, units / (q.tile <= LIN_TILE_ROWS64 ? 4 : 2))) : 1;
+    q.span = (units + n - 1) / n * 16;
+    q.nsplit = (ncb + q.span - 1) / q.span;
     q.ldw = (long long)nra * 32;
     return q;
 }
 
-// out[r][c .. c + 3] = epilogue(sum over the splits, in order); the weight
-// gradient's column sums likewise.
+// out[r][c .. c + 3] = epilogue(sum over the splits, in order).
 template <int OP>
 __global__ __launch_bounds__(256) void lin_join_kernel(const LinEpi e, const float* __restrict__ part, int nsplit,
-                                                       long long ldw, long long quads, const float* __restrict__ sums,
-                                                       float* __restrict__ colsum) {
+                                                       long long ldw, long long quads) {
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     if (i < quads) {
         const int per = (e.ncols + 3) / 4;
@@ -53,11 +52,6 @@ __global__ __launch_bounds__(256) void lin_join_kernel(const LinEpi e, const flo
         }
         lin_epilogue4<OP>(e, r, c, v);
     }
-    if (OP == LIN_WGRAD && colsum && i < e.nrows) {
-        float v = sums[i];
-        for (int k = 1; k < nsplit; k++) v += sums[(long long)k * e.nrows + i];
-        colsum[i] = v;
-    }
 }
 
 int lin_blocks(int n) { return (n + 31) / 32; }
@@ -67,7 +61,7 @@ int lin_blocks(int n) { return (n + 31) / 32; }
 size_t linear_workspace(int op, int nrows, int ncols, int ncon) {
     const LinPlan q = lin_plan(op, lin_blocks(ncols), lin_blocks(nrows), lin_blocks(ncon));
     if (q.nsplit == 1) return 0;
-    return (size_t)q.nsplit * ((size_t)nrows * q.ldw + (op == LIN_WGRAD ? nrows : 0)) * sizeof(float);
+    return (size_t)q.nsplit * (size_t)nrows * q.ldw * sizeof(float);
 }
 
 int launch_linear(int op, int fa, int fb, const LinMat& a, const LinMat& b, int ncon, const LinEpi& e, float* colsum,
@@ -83,23 +77,21 @@ int launch_linear(int op, int fa, int fb, const LinMat& a, const LinMat& b, int 
     p.a = {a.codes, a.scales, nra, ncb, ta ? ncb : 1, ta ? 1 : nra};
     p.b = {b.codes, b.scales, nrb, ncb, tb ? ncb : 1, tb ? 1 : nrb};
     p.e = e;
-    p.ta = q.ta; p.tb = q.tb; p.nsplit = q.nsplit; p.sps = q.sps;
+    p.ta = q.ta; p.tb = q.tb; p.nsplit = q.nsplit; p.span = q.span;
     p.ldw = q.ldw;
-    float* const sums = (float*)ws + (size_t)q.nsplit * e.nrows * q.ldw;
     p.part = q.nsplit > 1 ? (float*)ws : nullptr;
-    p.colsum = colsum && q.nsplit > 1 ? sums : colsum;
+    p.colsum = colsum;
+    p.nsum = colsum ? (nrb + 7) / 8 * 8 : 0;
     int rc;
     if (fa == MXC_E4M3) rc = launch_linear_e4m3(op, p, q.tile, s);
     else if (fa == MXC_E2M1 && fb == MXC_E2M1) rc = launch_linear_e2m1(op, p, q.tile, s);
     else rc = launch_linear_fp6(op, fa, fb, p, q.tile, s);
     if (rc || q.nsplit == 1) return rc;
     const long long quads = (long long)e.nrows * ((e.ncols + 3) / 4);
-    const long long nthr = std::max<long long>(quads, colsum ? e.nrows : 0);
-    const unsigned grid = (unsigned)((nthr + 255) / 256);
-    if (op == LIN_FWD) lin_join_kernel<LIN_FWD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads, sums, nullptr);
-    else if (op == LIN_DGRAD)
-        lin_join_kernel<LIN_DGRAD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads, sums, nullptr);
-    else lin_join_kernel<LIN_WGRAD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads, sums, colsum);
+    const unsigned grid = (unsigned)((quads + 255) / 256);
+    if (op == LIN_FWD) lin_join_kernel<LIN_FWD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads);
+    else if (op == LIN_DGRAD) lin_join_kernel<LIN_DGRAD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads);
+    else lin_join_kernel<LIN_WGRAD><<<grid, 256, 0, s>>>(e, p.part, q.nsplit, q.ldw, quads);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_HIP;
 }
 

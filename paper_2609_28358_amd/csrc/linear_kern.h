@@ -36,8 +36,8 @@ struct LinOp {
 // The epilogue: out[r][c] for output row r < nrows, column c < ncols.
 //   fwd    z = v + bias[c]; pre[r][c] = z; out = fn(z) + res[r][c]
 //   dgrad  out = v fn'(z[r][c]) + res[r][c]
-// pre doubles as dgrad's z.  vec: every pointer and stride allows vectors of
-// four columns, and ncols is a multiple of four.
+// pre doubles as dgrad's z.  vec: 1 where ncols and every stride allow vectors
+// of four columns, 2 where they allow 16 bytes.
 struct LinEpi {
     void* out;
     const float* bias;
@@ -59,9 +59,10 @@ struct LinArgs {
     LinEpi e;
     float* part;          // split contraction: partial sums [split][nrows][ldw], else NULL
     long long ldw;
-    float* colsum;        // weight gradient: db (or its partial sums [split][nrows]), or NULL
+    float* colsum;        // weight gradient: db, or NULL
+    int nsum;             // workgroups in front of the tiles that form it
     int ta, tb;           // tiles along A's and B's rows
-    int nsplit, sps;      // splits, stages of each
+    int nsplit, span;     // splits of the contraction, blocks of each (whole stages)
 };
 
 enum { LIN_FWD = 0, LIN_DGRAD = 1, LIN_WGRAD = 2 };
@@ -88,13 +89,16 @@ template <int FA, int FB, class T> struct LinLds {
     static constexpr int BBYTES = T::RB * T::KB * LinBlk<FB>::LDS;
     static constexpr int NSI = ((T::RA + T::RB) * T::KB + 63) / 64;          // scale copies of a stage
     static constexpr int STAGE = ABYTES + BBYTES + NSI * 256;
-    static constexpr int RED = T::WK > 1 ? T::W * T::MB * T::NB * 4096 : 0;  // joining the waves of the contraction
+    static constexpr int LD = 32 * T::MB + 4;                                // floats of an output row on its way out
+    // joining the waves of the contraction, or the waves' output rows
+    static constexpr int RED = T::WK > 1 ? T::W * T::MB * T::NB * 4096 : T::W * 32 * LD * 4;
     static constexpr int BYTES = T::NBUF * STAGE > RED ? T::NBUF * STAGE : RED;
 };
 
 // tile shapes a launch is asked for: outputs of at most 32 or 64 rows (the
-// contraction is shared by a workgroup's waves), 64 x 64, 128 x 128
-enum { LIN_TILE_ROWS32 = 0, LIN_TILE_ROWS64 = 1, LIN_TILE_64 = 2, LIN_TILE_128 = 3 };
+// contraction is shared by a workgroup's waves), 64 x 64, 128 x 128, 256
+// columns x 128 rows
+enum { LIN_TILE_ROWS32 = 0, LIN_TILE_ROWS64 = 1, LIN_TILE_64 = 2, LIN_TILE_128 = 3, LIN_TILE_256 = 4 };
 
 // linear.hip: workspace bytes and launch of one product (nrows x ncols
 // outputs over ncon, formats and matrices in the order A, B)
@@ -120,23 +124,28 @@ __device__ __forceinline__ void dma16_base(const uint8_t* base, uint32_t off, ui
 }
 
 // ---------------------------------------------------------------- epilogue
+// No contraction: every path (vectors, columns, joined splits) gives the same bits.
 template <int OP>
-__device__ __forceinline__ float lin_value(const LinEpi& e, float v, float b, float z, float r) {
+__device__ __forceinline__ float lin_value(int fn, float v, float b, float z, float r) {
+#pragma clang fp contract(off)
     if constexpr (OP == LIN_FWD) {
         v += b;
-        return (e.fn == MXC_FN_NONE ? v : e.fn == MXC_FN_RELU ? fn_apply_c<MXC_FN_RELU>(v) : fn_apply_c<MXC_FN_SILU>(v)) + r;
+        return (fn == MXC_FN_NONE ? v : fn == MXC_FN_RELU ? fn_apply_c<MXC_FN_RELU>(v) : fn_apply_c<MXC_FN_SILU>(v)) + r;
     } else if constexpr (OP == LIN_DGRAD) {
-        return (e.fn == MXC_FN_NONE ? v : v * fn_grad(e.fn, z)) + r;
+        return (fn == MXC_FN_NONE ? v : v * fn_grad(fn, z)) + r;
     } else {
         return v;
     }
 }
 
-__device__ __forceinline__ float4 lin_load4(const void* p, long long i, int bf16) {
-    return bf16 ? bf16_unpack4(*(const uint2*)((const uint16_t*)p + i)) : *(const float4*)((const float*)p + i);
+template <bool BF>
+__device__ __forceinline__ float4 lin_load4(const void* p, long long i) {
+    if constexpr (BF) return bf16_unpack4(*(const uint2*)((const uint16_t*)p + i));
+    else return *(const float4*)((const float*)p + i);
 }
-__device__ __forceinline__ void lin_store4(void* p, long long i, int bf16, float4 v) {
-    if (bf16) *(uint2*)((uint16_t*)p + i) = bf16_pack4(v.x, v.y, v.z, v.w);
+template <bool BF>
+__device__ __forceinline__ void lin_store4(void* p, long long i, float4 v) {
+    if constexpr (BF) *(uint2*)((uint16_t*)p + i) = bf16_pack4(v.x, v.y, v.z, v.w);
     else *(float4*)((float*)p + i) = v;
 }
 __device__ __forceinline__ float lin_load1(const void* p, long long i, int bf16) {
@@ -147,35 +156,154 @@ __device__ __forceinline__ void lin_store1(void* p, long long i, int bf16, float
     else ((float*)p)[i] = v;
 }
 
-// Four consecutive columns c .. c + 3 of output row r (r < nrows; columns past
-// ncols are dropped).  All arithmetic is fp32, rounded once where it is
-// stored; the activation is applied to the unrounded pre-activation.
+// Four consecutive columns c .. c + 3 of output row r, c + 3 < ncols, r <
+// nrows, as vectors (e.vec): what they read, and their results.  All
+// arithmetic is fp32, rounded once where it is stored; the activation is
+// applied to the unrounded pre-activation.
+struct LinAux {
+    float4 z, s;
+};
+template <int OP, bool BF>
+__device__ __forceinline__ LinAux lin_read4(const LinEpi& e, int r, int c) {
+    LinAux a;
+    a.z = a.s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (OP == LIN_FWD && e.bias) a.z = *(const float4*)(e.bias + c);
+    if (OP == LIN_DGRAD && e.fn != MXC_FN_NONE) a.z = lin_load4<BF>(e.pre, r * e.ldp + c);
+    if (OP != LIN_WGRAD && e.res) a.s = lin_load4<BF>(e.res, r * e.ldr + c);
+    return a;
+}
+template <int OP, bool BF>
+__device__ __forceinline__ void lin_write4(const LinEpi& e, int r, int c, float4 v, const LinAux& a) {
+    const float4 z = a.z, s = a.s;
+    if (OP == LIN_FWD && e.pre)
+        lin_store4<BF>(e.pre, r * e.ldp + c, make_float4(v.x + z.x, v.y + z.y, v.z + z.z, v.w + z.w));
+    // one uniform choice of the activation around four independent values
+    auto four = [&](int fn) {
+        lin_store4<BF>(e.out, r * e.ldo + c,
+                       make_float4(lin_value<OP>(fn, v.x, z.x, z.x, s.x), lin_value<OP>(fn, v.y, z.y, z.y, s.y),
+                                   lin_value<OP>(fn, v.z, z.z, z.z, s.z), lin_value<OP>(fn, v.w, z.w, z.w, s.w)));
+    };
+    if (OP == LIN_WGRAD || e.fn == MXC_FN_NONE) four(MXC_FN_NONE);
+    else if (e.fn == MXC_FN_RELU) four(MXC_FN_RELU);
+    else four(MXC_FN_SILU);
+}
+
+// Any alignment, column by column; columns past ncols are dropped.
+template <int OP>
+__device__ __forceinline__ void lin_scalar4(const LinEpi& e, int r, int c, float4 v) {
+    const float a[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        if (c + q >= e.ncols) return;
+        const float b = OP == LIN_FWD && e.bias ? e.bias[c + q] : 0.0f;
+        const float z = OP == LIN_DGRAD && e.fn != MXC_FN_NONE ? lin_load1(e.pre, r * e.ldp + c + q, e.bf16) : 0.0f;
+        const float s = OP != LIN_WGRAD && e.res ? lin_load1(e.res, r * e.ldr + c + q, e.bf16) : 0.0f;
+        if (OP == LIN_FWD && e.pre) lin_store1(e.pre, r * e.ldp + c + q, e.bf16, a[q] + b);
+        lin_store1(e.out, r * e.ldo + c + q, e.bf16, lin_value<OP>(e.fn, a[q], b, z, s));
+    }
+}
+
 template <int OP>
 __device__ __forceinline__ void lin_epilogue4(const LinEpi& e, int r, int c, float4 v) {
-    const float4 zero = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (e.vec) {
-        if (c >= e.ncols) return;
-        float4 b = zero, z = zero, s = zero;
-        if (OP == LIN_FWD && e.bias) b = *(const float4*)(e.bias + c);
-        if (OP == LIN_DGRAD && e.fn != MXC_FN_NONE) z = lin_load4(e.pre, r * e.ldp + c, e.bf16);
-        if (OP != LIN_WGRAD && e.res) s = lin_load4(e.res, r * e.ldr + c, e.bf16);
-        if (OP == LIN_FWD && e.pre)
-            lin_store4(e.pre, r * e.ldp + c, e.bf16, make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w));
-        lin_store4(e.out, r * e.ldo + c, e.bf16,
-                   make_float4(lin_value<OP>(e, v.x, b.x, z.x, s.x), lin_value<OP>(e, v.y, b.y, z.y, s.y),
-                               lin_value<OP>(e, v.z, b.z, z.z, s.z), lin_value<OP>(e, v.w, b.w, z.w, s.w)));
-    } else {
-        const float a[4] = {v.x, v.y, v.z, v.w};
+    if (!e.vec) lin_scalar4<OP>(e, r, c, v);
+    else if (c >= e.ncols) return;
+    else if (e.bf16) lin_write4<OP, true>(e, r, c, v, lin_read4<OP, true>(e, r, c));
+    else lin_write4<OP, false>(e, r, c, v, lin_read4<OP, false>(e, r, c));
+}
+
+// 16 bytes of a full-precision row: 8 bf16 or 4 fp32 columns.
+template <bool BF> constexpr int LIN_V = BF ? 8 : 4;
+template <bool BF>
+__device__ __forceinline__ void lin_unpack(uint4 u, float* o) {
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int q = 0; q < 4; q++) {
-            if (c + q >= e.ncols) return;
-            const float b = OP == LIN_FWD && e.bias ? e.bias[c + q] : 0.0f;
-            const float z = OP == LIN_DGRAD && e.fn != MXC_FN_NONE ? lin_load1(e.pre, r * e.ldp + c + q, e.bf16) : 0.0f;
-            const float s = OP != LIN_WGRAD && e.res ? lin_load1(e.res, r * e.ldr + c + q, e.bf16) : 0.0f;
-            if (OP == LIN_FWD && e.pre) lin_store1(e.pre, r * e.ldp + c + q, e.bf16, a[q] + b);
-            lin_store1(e.out, r * e.ldo + c + q, e.bf16, lin_value<OP>(e, a[q], b, z, s));
+    for (int k = 0; k < 4; k++) {
+        if constexpr (BF) {
+            o[2 * k] = __uint_as_float(w[k] << 16);
+            o[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+        } else {
+            o[k] = __uint_as_float(w[k]);
         }
     }
+}
+template <bool BF>
+__device__ __forceinline__ void lin_put(void* p, long long i, const float* v) {
+    if constexpr (BF) *(uint4*)((uint16_t*)p + i) = make_uint4(bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]),
+                                                               bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7]));
+    else *(float4*)((float*)p + i) = make_float4(v[0], v[1], v[2], v[3]);
+}
+template <bool BF>
+__device__ __forceinline__ uint4 lin_get(const void* p, long long i) {
+    return BF ? *(const uint4*)((const uint16_t*)p + i) : *(const uint4*)((const float*)p + i);
+}
+
+// One 32-row block of a wave (rows r0 .. r0 + 31, columns c0 .. c0 + 32 MB -
+// 1) on its way out through the wave's LDS rows: 16 bytes a lane, four rows'
+// reads in flight (a round trip to memory a batch is what bounded this part).
+// park() writes the block to LDS; the first batch's reads are issued before it.
+template <int OP, bool BF, int MB, class Park>
+__device__ __forceinline__ void lin_rows(const LinEpi& e, int r0, int c0, const float* mine, int lane, Park&& park) {
+    constexpr int V = LIN_V<BF>, LD = 32 * MB + 4;
+    constexpr int LPR = 32 * MB / V, RS = 64 / LPR, CNT = 32 / RS, BN = CNT < 4 ? CNT : 4;
+    const int row = lane / LPR, col = lane % LPR * V, c = c0 + col, cc = c < e.ncols ? c : 0;
+    const bool rd_z = OP == LIN_DGRAD && e.fn != MXC_FN_NONE, rd_s = OP != LIN_WGRAD && e.res;
+    uint4 z[BN], s[BN];
+    auto read = [&](int n) {
+#pragma unroll
+        for (int k = 0; k < BN; k++) {
+            const int r = min(r0 + row + (n + k) * RS, e.nrows - 1);
+            if (rd_z) z[k] = lin_get<BF>(e.pre, r * e.ldp + cc);
+            if (rd_s) s[k] = lin_get<BF>(e.res, r * e.ldr + cc);
+        }
+    };
+    read(0);
+    float b[V];
+#pragma unroll
+    for (int k = 0; k < V; k++) b[k] = 0.0f;
+    if (OP == LIN_FWD && e.bias) {
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+            const float4 u = *(const float4*)(e.bias + cc + k);
+            b[k] = u.x; b[k + 1] = u.y; b[k + 2] = u.z; b[k + 3] = u.w;
+        }
+    }
+    park();
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int n = 0; n < CNT; n += BN) {
+        if (n) read(n);
+        auto rows = [&](auto fn) {
+            constexpr int FN = decltype(fn)::fn;
+#pragma unroll
+            for (int k = 0; k < BN; k++) {
+                const int r = r0 + row + (n + k) * RS;
+                float v[V], zf[V], sf[V];
+#pragma unroll
+                for (int q = 0; q < V; q += 4) {
+                    const float4 u = *(const float4*)(mine + (row + (n + k) * RS) * LD + col + q);
+                    v[q] = u.x; v[q + 1] = u.y; v[q + 2] = u.z; v[q + 3] = u.w;
+                }
+#pragma unroll
+                for (int q = 0; q < V; q++) zf[q] = sf[q] = 0.0f;
+                if (FN != MXC_FN_NONE && OP == LIN_DGRAD) lin_unpack<BF>(z[k], zf);
+                if (rd_s) lin_unpack<BF>(s[k], sf);
+                if (r < e.nrows && c < e.ncols) {
+                    if (OP == LIN_FWD && e.pre) {
+#pragma unroll
+                        for (int q = 0; q < V; q++) zf[q] = v[q] + b[q];
+                        lin_put<BF>(e.pre, r * e.ldp + c, zf);
+                    }
+#pragma unroll
+                    for (int q = 0; q < V; q++) v[q] = lin_value<OP>(FN, v[q], b[q], zf[q], sf[q]);
+                    lin_put<BF>(e.out, r * e.ldo + c, v);
+                }
+            }
+        };
+        if (OP == LIN_WGRAD || e.fn == MXC_FN_NONE) rows(FnTag<MXC_FN_NONE>{});
+        else if (e.fn == MXC_FN_RELU) rows(FnTag<MXC_FN_RELU>{});
+        else rows(FnTag<MXC_FN_SILU>{});
+    }
+    __builtin_amdgcn_wave_barrier();
 }
 
 // ---------------------------------------------------------------- fragments
@@ -239,15 +367,76 @@ __device__ __forceinline__ void lin_wait(int later) {
     else vm_wait<2 * PER>();
 }
 
+// ---------------------------------------------------------------- column sums
+// db: the sums of dZ over its rows, for one of its column blocks -- a product
+// with a row of ones, exact like the others, from fragments that are contiguous
+// in memory.  The waves take pairs of row blocks in turn and are joined in
+// order.  (Taken along by the tiles of the weight gradient, the sums cost every
+// tile 16 or 32 registers: the 256 x 128 tile spilled and ran at a third.)
+template <int F, int W>
+__device__ __forceinline__ void lin_colsum(const LinOp& o, float* out, int n, int rb, float* red) {
+    constexpr int SRC = LinBlk<F>::SRC, ROW = SRC / 32;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (rb >= o.nrb) return;
+    v16f acc;
+#pragma unroll
+    for (int e = 0; e < 16; e++) acc[e] = 0.0f;
+    const int pairs = (o.ncb + 1) / 2;
+#pragma unroll 4
+    for (int p = wave; p < pairs; p += W) {
+        const int k0 = 2 * p, k1 = min(2 * p + 1, o.ncb - 1);
+        const bool two = 2 * p + 1 < o.ncb;
+        const size_t b0 = (size_t)rb * o.srow + (size_t)k0 * o.scon, b1 = (size_t)rb * o.srow + (size_t)k1 * o.scon;
+        const int s0 = o.scales[b0], s1 = two ? o.scales[b1] : 0;
+        v8i f;
+        if constexpr (F == MXC_E4M3) {
+            const int at = (lane & 31) * ROW + 16 * h;
+            const v4i u = *(const v4i*)(o.codes + b0 * SRC + at), w = *(const v4i*)(o.codes + b1 * SRC + at);
+#pragma unroll
+            for (int e = 0; e < 4; e++) { f[e] = u[e]; f[4 + e] = two ? w[e] : 0; }
+            uint32_t one[16], d[16];
+#pragma unroll
+            for (int e = 0; e < 16; e++) one[e] = 0x3F803F80u;
+            e4m3_decode32(f, s0, s1, d);
+            acc = mfma_x8(one, d, acc);
+        } else {
+            const uint8_t* q = o.codes + (h ? b1 : b0) * SRC + (lane & 31) * ROW;
+            const bool ok = two || !h;
+#pragma unroll
+            for (int e = 0; e < 8; e++) f[e] = 0;
+#pragma unroll
+            for (int e = 0; e < ROW / 8; e++) {
+                const v2i u = *(const v2i*)(q + 8 * e);
+                f[2 * e] = ok ? u[0] : 0;
+                f[2 * e + 1] = ok ? u[1] : 0;
+            }
+            v8i one;                              // E2M1 code 2 is 1.0
+#pragma unroll
+            for (int e = 0; e < 8; e++) one[e] = e < 4 ? 0x22222222 : 0;
+            acc = mfma_mx<MXC_E2M1, F>(one, f, acc, 127, h ? s1 : s0);
+        }
+    }
+    if (lane < 32) red[wave * 32 + lane] = acc[0];
+    __syncthreads();
+    if (threadIdx.x < 32 && rb * 32 + (int)threadIdx.x < n) {
+        float v = red[threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < W; w++) v += red[w * 32 + threadIdx.x];
+        out[rb * 32 + threadIdx.x] = v;
+    }
+}
+
 // ---------------------------------------------------------------- the product
 // A workgroup computes RA x RB blocks of 32 x 32 outputs.  A stage holds KB
 // contraction blocks of both operands, copied to LDS by global -> LDS loads
-// into a ring of NBUF stages, so NBUF - 2 stages are in flight while one is
-// multiplied; one barrier a stage publishes it and frees the stage before.
+// into a ring of NBUF stages: while one is multiplied the next is complete and
+// the two after it are in flight; one barrier a stage publishes the next and
+// frees the one before.
 // Row blocks past the end read the last one (their products are not stored);
 // contraction blocks past the end read zero codes and scales.
 template <int FA, int FB, int OP, class T>
-__global__ __launch_bounds__(T::W * 64) void linear_kernel(const LinArgs p) {
+__global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
     constexpr int MB = T::MB, NB = T::NB, WM = T::WM, WN = T::WN, WK = T::WK, KS = T::KS, NBUF = T::NBUF;
     constexpr int RA = T::RA, RB = T::RB, KB = T::KB, W = T::W;
     constexpr bool TA = OP == LIN_FWD, TB = OP != LIN_WGRAD;      // transposed reads
@@ -258,7 +447,7 @@ __global__ __launch_bounds__(T::W * 64) void linear_kernel(const LinArgs p) {
     constexpr int NA = RA * KB / BA::BPI, NSL = NA + RB * KB / BB::BPI;   // 1 KB copies of a stage
     constexpr int NQ = NSL / W, NSQ = (L::NSI + W - 1) / W, PER = NQ + NSQ;
     static_assert(NSL % W == 0 && RA * KB % BA::BPI == 0 && RB * KB % BB::BPI == 0 && KS % 2 == 0, "whole copies");
-    static_assert(NBUF >= 2 && NBUF <= 4, "ring");
+    static_assert(NBUF >= 3 && NBUF <= 5, "ring");
     static_assert(MB * NB <= 16, "accumulators");
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
 
@@ -268,7 +457,15 @@ __global__ __launch_bounds__(T::W * 64) void linear_kernel(const LinArgs p) {
     // contiguous run of tiles, so tiles that share an operand share its L2
     const int ntiles = p.ta * p.tb * p.nsplit;
     const int per = (ntiles + 7) / 8;
-    const int lin = (blockIdx.x % 8) * per + blockIdx.x / 8;
+    int bid = blockIdx.x;
+    if constexpr (OP == LIN_WGRAD) {
+        if (bid < p.nsum) {
+            lin_colsum<FB, W>(p.b, p.colsum, p.e.nrows, bid, (float*)smem);
+            return;
+        }
+        bid -= p.nsum;
+    }
+    const int lin = (bid % 8) * per + bid / 8;
     if (lin >= ntiles) return;
     // runs of up to 8 tiles along B inside a column of A's tiles
     const int split = lin / (p.ta * p.tb), t2 = lin - split * (p.ta * p.tb);
@@ -277,8 +474,8 @@ __global__ __launch_bounds__(T::W * 64) void linear_kernel(const LinArgs p) {
     const int ia = in_band / bw, ib = band * 8 + (in_band - ia * bw);
     const int ra0 = ia * RA, rb0 = ib * RB;
 
-    const int kbeg = split * p.sps * KB;
-    const int kend = min(p.a.ncb, kbeg + p.sps * KB);
+    const int kbeg = split * p.span;
+    const int kend = min(p.a.ncb, kbeg + p.span);
     const int nst = (kend - kbeg + KB - 1) / KB;
 
     // ---- this lane's part of each copy: block (row block, contraction block)
@@ -363,74 +560,76 @@ __global__ __launch_bounds__(T::W * 64) void linear_kernel(const LinArgs p) {
         for (int j = 0; j < NB; j++)
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.0f;
-    // weight gradient: the column sums of dZ are one more row of the product,
-    // with ones; the workgroups of the first tile along A take them
-    const bool sums = OP == LIN_WGRAD && p.colsum != nullptr && ia == 0 && wm == 0;
-    v16f csum[OP == LIN_WGRAD ? NB : 1];
-    if constexpr (OP == LIN_WGRAD) {
-#pragma unroll
-        for (int j = 0; j < NB; j++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) csum[j][e] = 0.0f;
-    }
+
+    // ---- the fragments of a step (two contraction blocks of each operand) are
+    // read from LDS one step ahead, each as soon as the registers of its
+    // predecessor are free, so the products do not wait for LDS.  X8: the raw
+    // codes are read ahead and decoded to bf16 in the step itself.
+    constexpr int STEPS = KS / 2;
+    v8i rawa[MB], rawb[NB];
+    int sca[MB][X8 ? 2 : 1], scb[NB][X8 ? 2 : 1];
+    auto scale = [&](const uint8_t* sc, int next, int* o) {
+        if constexpr (X8) {                       // a lane holds both blocks' codes
+            o[0] = *(const int*)sc;
+            o[1] = *(const int*)(sc + next);
+        } else {
+            o[0] = *(const int*)(sc + (lane >> 5) * next);
+        }
+    };
+    auto fetch_a = [&](const uint8_t* stage, int s, int i) {
+        const int k0 = wk * KS + 2 * s, ra = wm * MB + i;
+        rawa[i] = lin_frag<FA, TA>(stage + (TA ? ra * KB + k0 : k0 * RA + ra) * BA::LDS, (TA ? 1 : RA) * BA::LDS, lane);
+        scale(stage + L::ABYTES + L::BBYTES + 4 * (k0 * RA + ra), 4 * RA, sca[i]);
+    };
+    auto fetch_b = [&](const uint8_t* stage, int s, int j, v8i& raw, int* sc) {
+        const int k0 = wk * KS + 2 * s, rb = wn * NB + j;
+        raw = lin_frag<FB, TB>(stage + L::ABYTES + (TB ? rb * KB + k0 : k0 * RB + rb) * BB::LDS,
+                               (TB ? 1 : RB) * BB::LDS, lane);
+        scale(stage + L::ABYTES + L::BBYTES + 4 * (RA * KB + k0 * RB + rb), 4 * RB, sc);
+    };
 
     for (int j = 0; j < NBUF - 1 && j < nst; j++) issue(j);
+    lin_wait<PER>(min(NBUF - 2, nst - 1));
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NB; j++) fetch_b(smem, 0, j, rawb[j], scb[j]);
+#pragma unroll
+    for (int i = 0; i < MB; i++) fetch_a(smem, 0, i);
     int buf = 0;
     for (int st = 0; st < nst; st++) {
-        lin_wait<PER>(min(NBUF - 2, nst - 1 - st));
+        // stage st + 1 is complete for every wave, and stage st - 1's slot is free
+        if (st + 1 < nst) lin_wait<PER>(min(NBUF - 3, nst - 2 - st));
         __syncthreads();
         if (st + NBUF - 1 < nst) issue(buf == 0 ? NBUF - 1 : buf - 1);
-        const uint8_t* A = smem + buf * L::STAGE;
-        const uint8_t* B = A + L::ABYTES;
-        const uint8_t* SC = B + L::BBYTES;
+        const uint8_t* cur = smem + buf * L::STAGE;
         buf = buf + 1 == NBUF ? 0 : buf + 1;
+        // past the last stage the ring's old bytes are read and not used
+        const uint8_t* nxt = smem + buf * L::STAGE;
 #pragma unroll
-        for (int s = 0; s < KS / 2; s++) {
-            const int k0 = wk * KS + 2 * s;
-            auto blk = [&](bool tr, int R, int lds, int rb) {      // LDS offset of (row block rb, k0)
-                return (tr ? rb * KB + k0 : k0 * R + rb) * lds;
-            };
+        for (int s = 0; s < STEPS; s++) {
+            const uint8_t* ns = s + 1 < STEPS ? cur : nxt;
+            const int n = s + 1 < STEPS ? s + 1 : 0;
             v8i fb[NB];
             int sb[NB];
             uint32_t db[X8 ? NB : 1][16];
 #pragma unroll
             for (int j = 0; j < NB; j++) {
-                const int rb = wn * NB + j;
-                fb[j] = lin_frag<FB, TB>(B + blk(TB, RB, BB::LDS, rb), (TB ? 1 : RB) * BB::LDS, lane);
-                const uint8_t* sc = SC + 4 * (RA * KB + k0 * RB + rb);
-                if constexpr (X8) e4m3_decode32(fb[j], *(const int*)sc, *(const int*)(sc + 4 * RB), db[j]);
-                else sb[j] = *(const int*)(sc + (lane >> 5) * 4 * RB);
-            }
-            if constexpr (OP == LIN_WGRAD) {
-                if (sums) {
-#pragma unroll
-                    for (int j = 0; j < NB; j++) {
-                        if constexpr (X8) {
-                            uint32_t one[16];
-#pragma unroll
-                            for (int e = 0; e < 16; e++) one[e] = 0x3F803F80u;
-                            csum[j] = mfma_x8(one, db[j], csum[j]);
-                        } else {
-                            v8i one;      // E2M1 code 2 is 1.0
-#pragma unroll
-                            for (int e = 0; e < 8; e++) one[e] = e < 4 ? 0x22222222 : 0;
-                            csum[j] = mfma_mx<MXC_E2M1, FB>(one, fb[j], csum[j], 127, sb[j]);
-                        }
-                    }
-                }
+                if constexpr (X8) e4m3_decode32(rawb[j], scb[j][0], scb[j][1], db[j]);
+                else { fb[j] = rawb[j]; sb[j] = scb[j][0]; }
+                fetch_b(ns, n, j, rawb[j], scb[j]);
             }
 #pragma unroll
             for (int i = 0; i < MB; i++) {
-                const int ra = wm * MB + i;
-                const v8i fa = lin_frag<FA, TA>(A + blk(TA, RA, BA::LDS, ra), (TA ? 1 : RA) * BA::LDS, lane);
-                const uint8_t* sc = SC + 4 * (k0 * RA + ra);
                 if constexpr (X8) {
                     uint32_t da[16];
-                    e4m3_decode32(fa, *(const int*)sc, *(const int*)(sc + 4 * RA), da);
+                    e4m3_decode32(rawa[i], sca[i][0], sca[i][1], da);
+                    fetch_a(ns, n, i);
 #pragma unroll
                     for (int j = 0; j < NB; j++) acc[i][j] = mfma_x8(da, db[j], acc[i][j]);
                 } else {
-                    const int sa = *(const int*)(sc + (lane >> 5) * 4 * RA);
+                    const v8i fa = rawa[i];
+                    const int sa = sca[i][0];
+                    fetch_a(ns, n, i);
 #pragma unroll
                     for (int j = 0; j < NB; j++) acc[i][j] = mfma_mx<FA, FB>(fa, fb[j], acc[i][j], sa, sb[j]);
                 }
@@ -448,27 +647,42 @@ __global__ __launch_bounds__(T::W * 64) void linear_kernel(const LinArgs p) {
             lin_epilogue4<OP>(p.e, r, c, v);
         }
     };
-    if constexpr (OP == LIN_WGRAD) {
-        if (sums && WK == 1 && lane < 32) {
+    if constexpr (WK == 1) {
+        // One block row of B at a time through LDS, each wave in a region of
+        // its own, so that a row's MB blocks leave as one run: stored straight
+        // from the accumulators, every instruction would touch 32 rows with
+        // 16 (bf16) or 32 bytes each.  Rows are padded by four floats.
+        constexpr int LD = L::LD;
+        __syncthreads();                          // every wave is done with the ring
+        float* const mine = (float*)smem + wave * 32 * LD;
 #pragma unroll
-            for (int j = 0; j < NB; j++) {
-                const int r = (rb0 + wn * NB + j) * 32 + lane;
-                if (r < p.e.nrows) p.colsum[(size_t)split * p.e.nrows + r] = csum[j][0];
+        for (int j = 0; j < NB; j++) {
+            auto park = [&]() {
+#pragma unroll
+                for (int i = 0; i < MB; i++)
+#pragma unroll
+                    for (int q = 0; q < 4; q++)
+                        *(float4*)(mine + (lane & 31) * LD + 32 * i + 8 * q + 4 * (lane >> 5)) = make_float4(
+                            acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+            };
+            const int r0 = (rb0 + wn * NB + j) * 32, c0 = (ra0 + wm * MB) * 32;
+            if (p.part || p.e.vec < 2) {
+                park();
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+                for (int n = 0; n < 4 * MB; n++) {
+                    const int row = (n * 64 + lane) / (8 * MB), col = lane % (8 * MB) * 4;
+                    put(r0 + row, c0 + col, *(const float4*)(mine + row * LD + col));
+                }
+                __builtin_amdgcn_wave_barrier();
+            } else if (p.e.bf16) {
+                lin_rows<OP, true, MB>(p.e, r0, c0, mine, lane, park);
+            } else {
+                lin_rows<OP, false, MB>(p.e, r0, c0, mine, lane, park);
             }
         }
-    }
-    if constexpr (WK == 1) {
-#pragma unroll
-        for (int i = 0; i < MB; i++)
-#pragma unroll
-            for (int j = 0; j < NB; j++)
-#pragma unroll
-                for (int q = 0; q < 4; q++)
-                    put((rb0 + wn * NB + j) * 32 + (lane & 31), (ra0 + wm * MB + i) * 32 + 8 * q + 4 * (lane >> 5),
-                        make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]));
     } else {
         // the waves of one output block add their parts in order, through LDS
-        static_assert(OP != LIN_WGRAD || WK == 1, "column sums are not joined");
         __syncthreads();                          // every wave is done with the ring
         float4* red = (float4*)smem;              // [wk][wave of the tile][block][quad][lane]
         constexpr int BL = MB * NB * 256;         // float4s of a wave
@@ -511,7 +725,7 @@ int linear_launch(const LinArgs& a, hipStream_t s) {
         }
     }
     const long long tiles = (long long)a.ta * a.tb * a.nsplit;
-    kernel<<<(unsigned)((tiles + 7) / 8 * 8), T::W * 64, lds, s>>>(a);
+    kernel<<<(unsigned)((tiles + 7) / 8 * 8 + a.nsum), T::W * 64, lds, s>>>(a);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_HIP;
 }
 

@@ -642,7 +642,8 @@ static int linear_run(int op, const mxc_linear& p, int fa, int fb, const LinMat&
         !aligned16(e.out) || !aligned16(e.res) || !aligned16(e.pre) || !aligned16(e.bias) || !aligned16(colsum) ||
         (need && !aligned16(ws)))
         return MXC_ERR_ALIGN;
-    e.vec = e.ncols % 4 == 0 && e.ldo % 4 == 0 && (!e.res || e.ldr % 4 == 0) && (!e.pre || e.ldp % 4 == 0);
+    const long long all = e.ncols | e.ldo | (e.res ? e.ldr : 0) | (e.pre ? e.ldp : 0);   // its low bits: what divides all
+    e.vec = all % 4 ? 0 : e.bf16 && all % 8 ? 1 : 2;
     return launch_linear(op, fa, fb, a, b, ncon, e, colsum, ws, (hipStream_t)stream);
 }
 

@@ -280,29 +280,34 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(const N
     if (a.w_post) flush(s_post, a.p_post + bid * d);
 }
 
-// dst[k][c] = sum of n consecutive partial rows, in order: 32 columns a
-// workgroup, 8 threads a column taking every eighth row.
+// dst[k][c] = sum of n consecutive partial rows, in a fixed order: 32 columns a
+// workgroup, 32 threads a column, each taking every 32nd row, four loads at a
+// time.
 struct JoinArgs {
     const float* src[3];
     float* dst[3];
     int n[3], rows[3];            // partial rows of a result row, result rows
     int d;
 };
-__global__ __launch_bounds__(256) void norm_join_kernel(const JoinArgs a) {
-    __shared__ float red[8][32];
+__global__ __launch_bounds__(1024) void norm_join_kernel(const JoinArgs a) {
+    __shared__ float red[32][33];
     int job = 0, row = blockIdx.y;
     while (row >= a.rows[job]) row -= a.rows[job++];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), l = threadIdx.x >> 5;
-    const float* p = a.src[job] + (size_t)row * a.n[job] * a.d + c;
+    const int x = threadIdx.x & 31, l = threadIdx.x >> 5, c = blockIdx.x * 32 + x, n = a.n[job];
+    const float* p = a.src[job] + (size_t)row * n * a.d + min(c, a.d - 1);
     float s = 0.0f;
-    if (c < a.d)
-        for (int k = l; k < a.n[job]; k += 8) s += p[(size_t)k * a.d];
-    red[l][threadIdx.x & 31] = s;
-    __syncthreads();
-    if (l == 0 && c < a.d) {
+    for (int k = l; k < n; k += 128) {
+        float v[4];
 #pragma unroll
-        for (int k = 1; k < 8; k++) s += red[k][threadIdx.x];
-        a.dst[job][(size_t)row * a.d + c] = s;
+        for (int q = 0; q < 4; q++) v[q] = k + 32 * q < n ? p[(size_t)(k + 32 * q) * a.d] : 0.0f;
+        s += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    red[l][x] = s;
+    __syncthreads();
+    if (l == 0) {
+#pragma unroll
+        for (int k = 1; k < 32; k++) s += red[k][x];
+        if (c < a.d) a.dst[job][(size_t)row * a.d + c] = s;
     }
 }
 
@@ -394,7 +399,7 @@ int launch_norm_bwd(NormArgs a, bool bf16, bool vec, float* dw_pre, float* dw_po
     if (!nj) return MXC_OK;
     for (int k = nj; k < 3; k++) { j.src[k] = j.src[0]; j.dst[k] = j.dst[0]; j.n[k] = j.rows[k] = 0; }
     j.d = a.d;
-    norm_join_kernel<<<dim3((a.d + 31) / 32, nrows), 256, 0, s>>>(j);
+    norm_join_kernel<<<dim3((a.d + 31) / 32, nrows), 1024, 0, s>>>(j);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_HIP;
 }
 
