@@ -770,7 +770,7 @@ int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void
  *   norm       NULL, or device fp32 [1], written (0 for no elements).
  *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes.
  * The factor is read on the device: no synchronization.  count >= 0; a launch
- * takes 96 tensors, more take several.
+ * takes 448 tensors, more take several.
  * Errors: NULL, ARG, ALIGN, WORKSPACE, HIP. */
 typedef struct mxc_gtensor {
     const void* src;

@@ -5,7 +5,7 @@
 
 namespace mxc {
 
-constexpr int CLIP_TENSORS = 96;       // descriptors of a launch (kernel arguments)
+constexpr int CLIP_TENSORS = 448;      // descriptors of a launch (12.4 KB of kernel arguments)
 constexpr int CLIP_PARTS = 2048;       // partial sums of all launches
 
 int launch_grad_clip(int count, const mxc_gtensor* t, bool scale, double max_norm, float* norm, void* ws,

@@ -7,7 +7,7 @@
 // cannot be seen in an fp32 norm): at most 16 fp64 operations per 16 bytes,
 // far from that unit's rate.  A launch takes the descriptors of up to
 // CLIP_TENSORS tensors as kernel arguments; a workgroup finds the tensor of
-// its chunk by bisection over the chunk counts.  Each workgroup of the norm
+// its chunk by counting, lane by lane, the tensors that begin no later.  Each workgroup of the norm
 // leaves one partial sum; every workgroup of the scaling adds all of them, in
 // the same order, so the result does not depend on timing and there is no
 // third launch.
@@ -17,28 +17,36 @@
 namespace mxc {
 namespace {
 
-constexpr int CHUNK = 16384;           // bytes a workgroup takes at a time
 constexpr int CT = 256;
+constexpr int STEP = 4 * 16 * CT;      // bytes a workgroup has in flight: four vectors a thread
 
 struct ClipArgs {
     const void* src[CLIP_TENSORS];
     void* dst[CLIP_TENSORS];
     long long n[CLIP_TENSORS];         // elements; bit 62: bf16
     int first[CLIP_TENSORS + 1];       // first chunk of each tensor
-    int count, nblk;
+    int count, nblk, chunk;            // chunk: bytes a workgroup takes at a time, a multiple of STEP
 };
 constexpr long long BF16_BIT = 1ll << 62;
 
 // the tensor of chunk k: the last one whose first chunk is not past k (empty
-// tensors have no chunk and are stepped over)
+// tensors have no chunk and are stepped over), counted by the wave's lanes
 __device__ __forceinline__ int find_tensor(const ClipArgs& a, int k) {
-    int lo = 0, hi = a.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.first[mid] <= k) lo = mid;
-        else hi = mid;
-    }
-    return lo;
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int b = 0; b < a.count; b += 64)
+        n += __popcll(__ballot(b + lane < a.count && a.first[min(b + lane, a.count)] <= k));
+    return __builtin_amdgcn_readfirstlane(n - 1);
+}
+
+// body(16-byte offset in the chunk) for a workgroup's vectors, four at a time
+// and independent of each other, then tail(first byte, last byte) for what is left
+template <class Body, class Tail>
+__device__ __forceinline__ void vectors(int len, Body&& body, Tail&& tail) {
+    int o = threadIdx.x * 16;
+    for (; o + STEP - 16 * CT + 16 <= len; o += STEP) body(o, std::integral_constant<int, 4>{});
+    for (; o + 16 <= len; o += 16 * CT) body(o, std::integral_constant<int, 1>{});
+    if (o < len) tail(o, min(o + 16, len));
 }
 
 __device__ __forceinline__ double block_sum(double v, double* red) {
@@ -78,21 +86,22 @@ __global__ __launch_bounds__(CT) void clip_norm_kernel(const ClipArgs a, double*
         const int t = find_tensor(a, k);
         const bool bf = (a.n[t] & BF16_BIT) != 0;
         const long long n = a.n[t] & ~BF16_BIT, bytes = bf ? 2 * n : 4 * n;
-        const long long b0 = (long long)(k - a.first[t]) * CHUNK;
+        const long long b0 = (long long)(k - a.first[t]) * a.chunk;
         const uint8_t* p = (const uint8_t*)a.src[t] + b0;
-        const int len = (int)min((long long)CHUNK, bytes - b0);
+        const int len = (int)min((long long)a.chunk, bytes - b0);
+        vectors(len, [&](int o, auto num) {
+            constexpr int N = decltype(num)::value;
+            uint4 u[N];
 #pragma unroll
-        for (int i = 0; i < CHUNK / (16 * CT); i++) {
-            const int o = (i * CT + threadIdx.x) * 16;
-            if (o + 16 <= len) {
-                s += squares(*(const uint4*)(p + o), bf);
-            } else {
-                for (int q = o; q < len; q += bf ? 2 : 4) {
-                    const double v = bf ? __uint_as_float((uint32_t)*(const uint16_t*)(p + q) << 16) : *(const float*)(p + q);
-                    s += v * v;
-                }
+            for (int i = 0; i < N; i++) u[i] = *(const uint4*)(p + o + i * 16 * CT);
+#pragma unroll
+            for (int i = 0; i < N; i++) s += squares(u[i], bf);
+        }, [&](int o, int e) {
+            for (; o < e; o += bf ? 2 : 4) {
+                const double v = bf ? __uint_as_float((uint32_t)*(const uint16_t*)(p + o) << 16) : *(const float*)(p + o);
+                s += v * v;
             }
-        }
+        });
     }
     s = block_sum(s, red);
     if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -108,35 +117,38 @@ __global__ __launch_bounds__(CT) void clip_scale_kernel(const ClipArgs a, const 
     const double ratio = max_norm / (norm + 1e-6);
     const float c = (float)(ratio >= 1.0 ? 1.0 : ratio);       // NaN stays NaN
     const int chunks = a.first[a.count];
-    for (int k = blockIdx.x; k < chunks; k += gridDim.x) {
+    // from the back: what the norm read last is still in the last-level cache
+    for (int k = chunks - 1 - (int)blockIdx.x; k >= 0; k -= gridDim.x) {
         const int t = find_tensor(a, k);
         const bool bf = (a.n[t] & BF16_BIT) != 0;
         if (a.src[t] == a.dst[t] && c == 1.0f) continue;       // already what it is scaled to
         const long long n = a.n[t] & ~BF16_BIT, bytes = bf ? 2 * n : 4 * n;
-        const long long b0 = (long long)(k - a.first[t]) * CHUNK;
+        const long long b0 = (long long)(k - a.first[t]) * a.chunk;
         const uint8_t* p = (const uint8_t*)a.src[t] + b0;
-        uint8_t* o = (uint8_t*)a.dst[t] + b0;
-        const int len = (int)min((long long)CHUNK, bytes - b0);
+        uint8_t* d = (uint8_t*)a.dst[t] + b0;
+        const int len = (int)min((long long)a.chunk, bytes - b0);
+        vectors(len, [&](int o, auto num) {
+            constexpr int N = decltype(num)::value;
+            uint4 u[N];
 #pragma unroll
-        for (int i = 0; i < CHUNK / (16 * CT); i++) {
-            const int at = (i * CT + threadIdx.x) * 16;
-            if (at + 16 <= len) {
-                const uint4 u = *(const uint4*)(p + at);
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            for (int i = 0; i < N; i++) u[i] = *(const uint4*)(p + o + i * 16 * CT);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
                 uint32_t r[4];
 #pragma unroll
                 for (int q = 0; q < 4; q++)
                     r[q] = bf ? bf16_pack2(__uint_as_float(w[q] << 16) * c, __uint_as_float(w[q] & 0xFFFF0000u) * c)
                               : __float_as_uint(__uint_as_float(w[q]) * c);
-                *(uint4*)(o + at) = make_uint4(r[0], r[1], r[2], r[3]);
-            } else {
-                for (int q = at; q < len; q += bf ? 2 : 4) {
-                    if (bf) *(uint16_t*)(o + q) =
-                        (uint16_t)bf16_bits(__uint_as_float((uint32_t)*(const uint16_t*)(p + q) << 16) * c);
-                    else *(float*)(o + q) = *(const float*)(p + q) * c;
-                }
+                *(uint4*)(d + o + i * 16 * CT) = make_uint4(r[0], r[1], r[2], r[3]);
             }
-        }
+        }, [&](int o, int e) {
+            for (; o < e; o += bf ? 2 : 4) {
+                if (bf) *(uint16_t*)(d + o) =
+                    (uint16_t)bf16_bits(__uint_as_float((uint32_t)*(const uint16_t*)(p + o) << 16) * c);
+                else *(float*)(d + o) = *(const float*)(p + o) * c;
+            }
+        });
     }
 }
 
@@ -146,8 +158,13 @@ int launch_grad_clip(int count, const mxc_gtensor* t, bool scale, double max_nor
                      hipStream_t s) {
     const int launches = std::max(1, (count + CLIP_TENSORS - 1) / CLIP_TENSORS);
     const int most = std::max(1, CLIP_PARTS / launches);
+    // long chunks spread a workgroup's search over more bytes, short ones fill
+    // the grid; either way a multiple of what is in flight
+    double total = 0.0;
+    for (int i = 0; i < count; i++) total += (double)t[i].n * (t[i].dtype == MXC_BF16 ? 2 : 4);
     int at = 0;
     ClipArgs a;
+    a.chunk = total > 256e6 ? 4 * STEP : STEP;
     auto table = [&](int l) {
         a.count = 0;
         a.first[0] = 0;
@@ -157,7 +174,7 @@ int launch_grad_clip(int count, const mxc_gtensor* t, bool scale, double max_nor
             a.src[k] = t[i].src;
             a.dst[k] = t[i].dst;
             a.n[k] = t[i].n | (bf ? BF16_BIT : 0);
-            a.first[k + 1] = a.first[k] + (int)((t[i].n * (bf ? 2 : 4) + CHUNK - 1) / CHUNK);
+            a.first[k + 1] = a.first[k] + (int)((t[i].n * (bf ? 2 : 4) + a.chunk - 1) / a.chunk);
         }
         if (a.count == 0) { a.count = 1; a.src[0] = a.dst[0] = nullptr; a.n[0] = 0; a.first[1] = 0; }
         a.nblk = std::max(1, std::min(most, a.first[a.count]));
@@ -169,9 +186,9 @@ int launch_grad_clip(int count, const mxc_gtensor* t, bool scale, double max_nor
         if (hipGetLastError() != hipSuccess) return MXC_ERR_HIP;
     }
     // without outputs, one workgroup writes the norm
-    for (int l = 0; l < (scale ? launches : 1); l++) {
+    for (int l = scale ? launches - 1 : 0; l >= 0; l--) {
         table(l);
-        if (!scale) a.first[a.count] = 0;
+        if (!scale) a.count = 0, a.first[0] = 0;
         clip_scale_kernel<<<scale ? a.nblk : 1, CT, 0, s>>>(a, (const double*)ws, at, max_norm, l == 0 ? norm : nullptr);
         if (hipGetLastError() != hipSuccess) return MXC_ERR_HIP;
     }

@@ -10,7 +10,7 @@ import ctypes
 import functools
 import os
 from array import array
-from operator import itemgetter
+from operator import attrgetter, itemgetter
 
 import torch
 
@@ -601,7 +601,8 @@ def _place(device, stream):
         if stream.device != device:
             raise MxconvError(f"the stream is on {stream.device}, the tensors on {device}")
         return torch.cuda.stream(stream)
-    return _here if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    here = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    return _here if device.index == here else torch.cuda.device(device)
 
 
 def _rows_cols(t, what, rows, cols, dtype, device):
@@ -750,6 +751,13 @@ def _norm_struct(y, w_post, gate, scale, w_pre, eps):
     return MxcNorm(rows, gates, d, _DTYPES[y.dtype], scale, eps, _ptr(w_post), _ptr(gate), _ptr(w_pre)), gates
 
 
+@functools.lru_cache(maxsize=_CACHED)
+def _norm_workspace_bytes(rows, gates, d, gate, post, pre):
+    some = 16                                         # only whether a pointer is NULL is looked at
+    s = MxcNorm(rows, gates, d, F32, 1.0, 0.0, some if post else None, some if gate else None, some if pre else None)
+    return lib().mxconv_norm_workspace_bytes(ctypes.byref(s))
+
+
 def norm_residual(x, y, w_post=None, gate=None, scale=1.0, w_pre=None, eps=1e-6, h_out=None, u_out=None, stream=None):
     """(H, U): H = x + scale * gate . N(y; w_post) and U = N(H; w_pre), N(v; w)
     = w . v / sqrt(mean(v^2) + eps) by rows (mxconv_norm_fwd).  x, y: [rows][d],
@@ -788,42 +796,68 @@ def norm_residual_backward(dh, du, h, y, w_post=None, gate=None, scale=1.0, w_pr
         lddx, lddy = _rows_cols(dx, "dx_out", rows, d, dt, dev), _rows_cols(dy, "dy_out", rows, d, dt, dev)
         dw_pre, dw_post, dgate = (torch.empty(sh, dtype=torch.float32, device=dev) if t is not None else None
                                   for t, sh in ((w_pre, (d,)), (w_post, (d,)), (gate, (gates, d))))
-        ws, wp, wb = _workspace(workspace, lib().mxconv_norm_workspace_bytes(ctypes.byref(s)), dev)
+        ws, wp, wb = _workspace(workspace, _norm_workspace_bytes(rows, gates, d, gate is not None, w_post is not None,
+                                                                 w_pre is not None), dev)
         _check(lib().mxconv_norm_bwd(ctypes.byref(s), _ptr(dh), lds[0], _ptr(du), lds[1], _ptr(h), lds[2], _ptr(y), lds[3],
                                      _ptr(dx), lddx, _ptr(dy), lddy, _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), wp, wb,
                                      _stream(stream)), "mxconv_norm_bwd")
     return dx, dy, dw_pre, dw_post, dgate
 
 
+def _descriptors(tensors, dev):
+    """Pointers, sizes and types of contiguous fp32 / bf16 tensors on device
+    `dev`, a list each (by map(): a step has hundreds of tensors)."""
+    types = list(map(_dtype_of, tensors))
+    if not set(types) <= _DTYPES.keys() or set(map(torch.Tensor.get_device, tensors)) != {dev.index} or \
+            not all(map(torch.Tensor.is_contiguous, tensors)):
+        raise MxconvError(f"gradients and their outputs must be contiguous fp32 or bf16 tensors on {dev}")
+    return list(map(torch.Tensor.data_ptr, tensors)), list(map(torch.Tensor.numel, tensors)), types
+
+
+_dtype_of = attrgetter("dtype")
+
+
 def _clip(tensors, outs, max_norm, norm_out, workspace, stream):
     if not tensors:
         raise MxconvError("no tensors")
     dev = tensors[0].device
-    desc = array("q")
-    for t, o in zip(tensors, outs if outs is not None else tensors):
-        code = _DTYPES.get(t.dtype)
-        if code is None or t.device != dev or not t.is_contiguous():
-            raise MxconvError(f"gradients must be contiguous fp32 or bf16 tensors on {dev}")
-        n = t.numel()
-        if o is not t and (o.dtype != t.dtype or o.numel() != n or o.device != dev or not o.is_contiguous()):
-            raise MxconvError("an output must be contiguous and have its gradient's size, type and device")
-        desc.extend((t.data_ptr(), o.data_ptr() if outs is not None else 0, n, code))
-    written = [p for p, n in zip(desc[1::4], desc[2::4]) if p and n]
-    if len(set(written)) != len(written):
-        raise MxconvError("a tensor is written twice")
+    if dev.type != "cuda":
+        raise MxconvError(f"tensors must be on a GPU, got {dev}")
+    ptrs, sizes, types = _descriptors(tensors, dev)
+    desc = array("q", bytes(32 * len(ptrs)))          # mxc_gtensor: src, dst, n, dtype
+    desc[0::4] = array("q", ptrs)
+    desc[2::4] = array("q", sizes)
+    desc[3::4] = array("q", map(_DTYPES.get, types))
+    if outs is not None:
+        dst = ptrs
+        if outs is not tensors:
+            outs = list(outs)
+            if len(outs) != len(tensors):
+                raise MxconvError(f"{len(outs)} outputs for {len(tensors)} tensors")
+            dst, osizes, otypes = _descriptors(outs, dev)
+            if osizes != sizes or otypes != types:
+                raise MxconvError("an output must have its gradient's size and type")
+        desc[1::4] = array("q", dst)
+        if len(set(dst)) != len(dst) and len(set(full := [p for p, n in zip(dst, sizes) if n])) != len(full):
+            raise MxconvError("a tensor is written twice")
     with _place(dev, stream):
         norm = norm_out if norm_out is not None else torch.empty((), dtype=torch.float32, device=dev)
         if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != dev:
             raise MxconvError(f"norm_out must be one fp32 element on {dev}")
-        ws, wp, wb = _workspace(workspace, lib().mxconv_grad_clip_workspace_bytes(), dev)
-        _check(lib().mxconv_grad_clip(len(tensors), desc.buffer_info()[0], max_norm, _ptr(norm), wp, wb, _stream(stream)),
+        ws, wp, wb = _workspace(workspace, _clip_workspace_bytes(), dev)
+        _check(lib().mxconv_grad_clip(len(ptrs), desc.buffer_info()[0], max_norm, _ptr(norm), wp, wb, _stream(stream)),
                "mxconv_grad_clip")
     return norm
 
 
+@functools.lru_cache(maxsize=None)
+def _clip_workspace_bytes():
+    return lib().mxconv_grad_clip_workspace_bytes()
+
+
 def grad_norm(tensors, norm_out=None, workspace=None, stream=None):
     """The Euclidean norm of all elements of the tensors, an fp32 device scalar."""
-    return _clip(tensors, None, float("inf"), norm_out, workspace, stream)
+    return _clip(list(tensors), None, float("inf"), norm_out, workspace, stream)
 
 
 def grad_clip(tensors, max_norm, out=None, norm_out=None, workspace=None, stream=None):
@@ -831,8 +865,7 @@ def grad_clip(tensors, max_norm, out=None, norm_out=None, workspace=None, stream
     1e-6)), norm = their Euclidean norm together, into `out` (tensors of the
     same sizes and types; None: in place).  Returns the norm before scaling, an
     fp32 device scalar; nothing is synchronized (mxconv_grad_clip)."""
-    if out is not None and len(out) != len(tensors):
-        raise MxconvError(f"{len(out)} outputs for {len(tensors)} tensors")
+    tensors = list(tensors)
     return _clip(tensors, tensors if out is None else out, max_norm, norm_out, workspace, stream)
 
 
