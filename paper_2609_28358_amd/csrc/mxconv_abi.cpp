@@ -2,7 +2,6 @@
 // size helpers and dispatch to the gfx950 kernels.  Every argument check runs
 // on the host before anything is enqueued.
 #include <cmath>
-#include <initializer_list>
 #include <mutex>
 
 #include "clip.h"
@@ -715,15 +714,6 @@ static NormArgs norm_args(const mxc_norm& p) {
     return a;
 }
 
-// 16-byte vectors: the row length and every stride in use a multiple of them
-static bool norm_vec(const mxc_norm& p, std::initializer_list<int64_t> strides) {
-    const int v = p.dtype == MXC_BF16 ? 8 : 4;
-    if (p.d % v) return false;
-    for (int64_t s : strides)
-        if (s % v) return false;
-    return true;
-}
-
 int mxconv_norm_fwd(const mxc_norm* p, const void* x, int64_t ldx, const void* y, int64_t ldy, void* h, int64_t ldh,
                     void* u, int64_t ldu, void* stream) {
     if (!p || !x || !y || !h || (p->w_pre && !u)) return MXC_ERR_NULL;
@@ -738,8 +728,7 @@ int mxconv_norm_fwd(const mxc_norm* p, const void* x, int64_t ldx, const void* y
     NormArgs a = norm_args(*p);
     a.x = x; a.y = y; a.h = h; a.u = u;
     a.ldx = ldx; a.ldy = ldy; a.ldh = ldh; a.ldu = ldu;
-    const bool vec = norm_vec(*p, {ldx, ldy, ldh, p->w_pre ? ldu : 0});
-    return launch_norm_fwd(a, p->dtype == MXC_BF16, vec, (hipStream_t)stream);
+    return launch_norm_fwd(a, p->dtype == MXC_BF16, (hipStream_t)stream);
 }
 
 size_t mxconv_norm_workspace_bytes(const mxc_norm* p) {
@@ -768,8 +757,7 @@ int mxconv_norm_bwd(const mxc_norm* p, const void* dh, int64_t lddh, const void*
     a.x = dh; a.y = y; a.h = const_cast<void*>(h); a.u = const_cast<void*>(du);
     a.dx = dx; a.dy = dy;
     a.ldx = lddh; a.ldy = ldy; a.ldh = ldh; a.ldu = lddu; a.lddx = lddx; a.lddy = lddy;
-    const bool vec = norm_vec(*p, {lddh, ldy, p->w_pre ? ldh : 0, p->w_pre ? lddu : 0, lddx, lddy});
-    return launch_norm_bwd(a, p->dtype == MXC_BF16, vec, dw_pre, dw_post, dgate, workspace, (hipStream_t)stream);
+    return launch_norm_bwd(a, p->dtype == MXC_BF16, dw_pre, dw_post, dgate, workspace, (hipStream_t)stream);
 }
 
 // ---- gradient clipping

@@ -5,13 +5,24 @@
 
 namespace mxc {
 
-constexpr int NORM_VALS = 16;          // values of a row a thread holds
 constexpr int NORM_MAX_DIM = 8192;
-constexpr int NORM_RUNS = 1024;        // backward: workgroups, so partial column sums
 constexpr int NORM_FWD_RUNS = 4096;
 
-// threads that share a row
-inline int norm_tpr(int d) { return d <= 64 * NORM_VALS ? 64 : d <= 256 * NORM_VALS ? 256 : 512; }
+// Threads that share a row, and the values of it that each holds: 8, so that
+// four waves a SIMD fit, but 16 for the longest rows (a row of 8192 on 1024
+// threads of 8 ran at 3.3, on 512 of 16 at 3.8 TB/s forward).
+inline int norm_vals(int d) { return d <= 4096 ? 8 : 16; }
+inline int norm_tpr(int d) {
+    int t = 64;
+    while (t * norm_vals(d) < d) t *= 2;
+    return t;
+}
+// rows a workgroup takes at a time: forward workgroups are a row's threads (at
+// least 256), backward ones 512, for fewer partial sums
+inline int norm_fwd_rows(int d) { return norm_tpr(d) == 64 ? 4 : 1; }
+inline int norm_bwd_rows(int d) { return 512 / norm_tpr(d); }
+// backward workgroups, so partial column sums: what the CUs hold at once
+inline int norm_runs(int d) { return norm_vals(d) == 8 ? 512 : 256; }
 
 struct NormArgs {
     const void* x;                     // forward X, backward dH
@@ -24,17 +35,17 @@ struct NormArgs {
     const float* w_post;
     const float* w_pre;
     const float* gate;                 // [gates][d], gate r / gate_rows for row r
-    float* p_pre;                      // partial column sums [runs][d]
-    float* p_post;
-    float* p_gate;                     // [runs][d], or dgate itself
+    float* p_pre;                      // partial column sums [runs][d]: of du hh,
+    float* p_c;                        // of dX yh, for runs inside one gate's rows;
+    float* p_post;                     // else dw_post's, of whole gates,
+    float* p_gate;                     // and dgate itself
     long long rows, gates, gate_rows, run, runs, runs_per_gate, gates_per_run;
     int d;
     float scale, eps, inv_d;
 };
 
-int launch_norm_fwd(NormArgs a, bool bf16, bool vec, hipStream_t s);
+int launch_norm_fwd(NormArgs a, bool bf16, hipStream_t s);
 size_t norm_bwd_workspace(long long rows, int d, long long gates, bool gate, bool post, bool pre);
-int launch_norm_bwd(NormArgs a, bool bf16, bool vec, float* dw_pre, float* dw_post, float* dgate, void* ws,
-                    hipStream_t s);
+int launch_norm_bwd(NormArgs a, bool bf16, float* dw_pre, float* dw_post, float* dgate, void* ws, hipStream_t s);
 
 }  // namespace mxc

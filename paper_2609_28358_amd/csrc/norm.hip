@@ -21,49 +21,79 @@
 namespace mxc {
 namespace {
 
-constexpr int NV = NORM_VALS;     // values of a row a thread holds
+// A thread's vector of a row: 16 bytes (8 bf16 or 4 fp32), V values.  Rows of
+// any length and stride are read and written with it: global memory takes
+// 16-byte accesses at any element's address, so only the last, partial vector of
+// a row goes element by element.  Values past the row's end are zeros, which no
+// sum sees.
+template <typename T> constexpr int VEC = 16 / (int)sizeof(T);
+struct __attribute__((packed, aligned(2))) Raw16 {
+    uint32_t w[4];
+};
+struct __attribute__((packed, aligned(4))) Raw16f {
+    uint32_t w[4];
+};
+template <typename T> using Raw = std::conditional_t<sizeof(T) == 2, Raw16, Raw16f>;
 
-template <typename T, int V>
-__device__ __forceinline__ void ld(const T* p, float* o) {
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (V == 4) {
-            const float4 u = *(const float4*)p;
-            o[0] = u.x; o[1] = u.y; o[2] = u.z; o[3] = u.w;
-        } else {
-            o[0] = *p;
-        }
-    } else if constexpr (V == 8) {
-        const uint4 u = *(const uint4*)p;
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+template <typename T>
+__device__ __forceinline__ float ld1(const T* p) {
+    if constexpr (sizeof(T) == 4) return *p;
+    else return __uint_as_float((uint32_t)*(const uint16_t*)p << 16);
+}
+template <typename T>
+__device__ __forceinline__ void st1(T* p, float v) {
+    if constexpr (sizeof(T) == 4) *p = v;
+    else *(uint16_t*)p = (uint16_t)bf16_bits(v);
+}
+// n: values of the row left from here on
+template <typename T>
+__device__ __forceinline__ void ld(const T* p, int n, float* o) {
+    constexpr int V = VEC<T>;
+    if (n >= V) {
+        const Raw<T> u = *(const Raw<T>*)p;
 #pragma unroll
         for (int k = 0; k < 4; k++) {
-            o[2 * k] = __uint_as_float(w[k] << 16);
-            o[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+            if constexpr (V == 8) {
+                o[2 * k] = __uint_as_float(u.w[k] << 16);
+                o[2 * k + 1] = __uint_as_float(u.w[k] & 0xFFFF0000u);
+            } else {
+                o[k] = __uint_as_float(u.w[k]);
+            }
         }
     } else {
-        o[0] = __uint_as_float((uint32_t)*(const uint16_t*)p << 16);
+#pragma unroll
+        for (int e = 0; e < V; e++) o[e] = e < n ? ld1(p + e) : 0.0f;
     }
 }
-template <typename T, int V>
-__device__ __forceinline__ void st(T* p, const float* v) {
-    if constexpr (sizeof(T) == 4) {
-        if constexpr (V == 4) *(float4*)p = make_float4(v[0], v[1], v[2], v[3]);
-        else *p = v[0];
-    } else if constexpr (V == 8) {
-        *(uint4*)p = make_uint4(bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]), bf16_pack2(v[4], v[5]),
-                                bf16_pack2(v[6], v[7]));
+template <typename T>
+__device__ __forceinline__ void st(T* p, int n, const float* v) {
+    constexpr int V = VEC<T>;
+    if (n >= V) {
+        Raw<T> u;
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+            if constexpr (V == 8) u.w[k] = bf16_pack2(v[2 * k], v[2 * k + 1]);
+            else u.w[k] = __float_as_uint(v[k]);
+        }
+        *(Raw<T>*)p = u;
     } else {
-        *(uint16_t*)p = (uint16_t)bf16_bits(v[0]);
+#pragma unroll
+        for (int e = 0; e < V; e++)
+            if (e < n) st1(p + e, v[e]);
     }
 }
 // V consecutive fp32 parameters
 template <int V>
-__device__ __forceinline__ void ldp(const float* p, float* o) {
+__device__ __forceinline__ void ldp(const float* p, int n, float* o) {
+    ld<float>(p, n, o);
+    if constexpr (V == 8) ld<float>(n > 4 ? p + 4 : p, max(n - 4, 0), o + 4);
+}
+
+template <int V>
+__device__ __forceinline__ void stp(float* p, int n, const float* v) {
+    st<float>(p, n, v);
     if constexpr (V == 8) {
-        ld<float, 4>(p, o);
-        ld<float, 4>(p + 4, o + 4);
-    } else {
-        ld<float, V>(p, o);
+        if (n > 4) st<float>(p + 4, n - 4, v + 4);
     }
 }
 
@@ -80,7 +110,7 @@ __device__ __forceinline__ void row_sum(float* v, float (*both)[N], int& par) {
         constexpr int W = TPR / 64;
         float* red = both[par];
         par ^= 1;
-        const int wave = threadIdx.x >> 6;
+        const int wave = threadIdx.x >> 6, first = wave / W * W;
         if ((threadIdx.x & 63) == 0) {
 #pragma unroll
             for (int k = 0; k < K; k++) red[wave * K + k] = v[k];
@@ -91,48 +121,49 @@ __device__ __forceinline__ void row_sum(float* v, float (*both)[N], int& par) {
 #pragma unroll
         for (int w = 0; w < W; w++)
 #pragma unroll
-            for (int k = 0; k < K; k++) v[k] += red[w * K + k];
+            for (int k = 0; k < K; k++) v[k] += red[(first + w) * K + k];
     }
 }
 
-// The value q of a thread is column (q / V) * TPR * V + t * V + q % V.
-template <int V, int TPR, class F>
+// The value q (of NV) of a thread is column (q / V) * TPR * V + t * V + q % V.
+template <int V, int NV, int TPR, class F>
 __device__ __forceinline__ void columns(int d, int t, F&& f) {
 #pragma unroll
     for (int i = 0; i < NV / V; i++) {
         const int c = (i * TPR + t) * V;
-        if (i * TPR * V < d && c < d) f(i * V, c);
+        if (i * TPR * V < d && c < d) f(i * V, c, d - c);
     }
 }
 
-template <typename T, int V, int TPR>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const NormArgs a) {
-    constexpr int RL = TPR < 256 ? 256 / TPR : 1;             // rows a workgroup takes at a time
+template <typename T, int NV, int TPR>
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NV == 8 ? 4 : 2) void norm_fwd_kernel(const NormArgs a) {
+    constexpr int V = VEC<T>;
+    constexpr int RL = TPR == 64 ? 4 : 1;             // rows a workgroup takes at a time
     __shared__ float red[2][TPR / 64];
     int par = 0;
     const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR, d = a.d;
     const long long first = (long long)blockIdx.x * a.run, last = min(first + a.run, a.rows);
     float wp[NV], wq[NV], g[NV];
-    columns<V, TPR>(d, t, [&](int q, int c) {
-        if (a.w_post) ldp<V>(a.w_post + c, wp + q);
-        if (a.w_pre) ldp<V>(a.w_pre + c, wq + q);
+    columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
+        if (a.w_post) ldp<V>(a.w_post + c, n, wp + q);
+        if (a.w_pre) ldp<V>(a.w_pre + c, n, wq + q);
     });
     long long gate = -1;
     for (long long r = first + rl; r < last; r += RL) {
         const long long gr = a.gate ? r / a.gate_rows : 0;
-        if (gr != gate) {                                     // the weights times s g, for this gate's rows
+        if (gr != gate) {                                     // s g, for this gate's rows
             gate = gr;
-            columns<V, TPR>(d, t, [&](int q, int c) {
+            columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
                 float u[V];
-                if (a.gate) ldp<V>(a.gate + gr * d + c, u);
+                if (a.gate) ldp<V>(a.gate + gr * d + c, n, u);
 #pragma unroll
                 for (int e = 0; e < V; e++) g[q + e] = a.gate ? a.scale * u[e] : a.scale;
             });
         }
         float x[NV], y[NV], s[1] = {0.0f};
-        columns<V, TPR>(d, t, [&](int q, int c) {
-            ld<T, V>((const T*)a.x + r * a.ldx + c, x + q);
-            ld<T, V>((const T*)a.y + r * a.ldy + c, y + q);
+        columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
+            ld<T>((const T*)a.x + r * a.ldx + c, n, x + q);
+            ld<T>((const T*)a.y + r * a.ldy + c, n, y + q);
 #pragma unroll
             for (int e = 0; e < V; e++) s[0] += y[q + e] * y[q + e];
         });
@@ -142,92 +173,99 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_fwd_kernel(const N
             ry = 1.0f / sqrtf(s[0] * a.inv_d + a.eps);
         }
         s[0] = 0.0f;
-        columns<V, TPR>(d, t, [&](int q, int c) {
+        columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
 #pragma unroll
             for (int e = 0; e < V; e++) {
-                const float n = a.w_post ? y[q + e] * ry * wp[q + e] : y[q + e];
-                x[q + e] += g[q + e] * n;
+                const float v = a.w_post ? y[q + e] * ry * wp[q + e] : y[q + e];
+                x[q + e] += g[q + e] * v;
                 s[0] += x[q + e] * x[q + e];
             }
-            st<T, V>((T*)a.h + r * a.ldh + c, x + q);
+            st<T>((T*)a.h + r * a.ldh + c, n, x + q);
         });
         if (a.w_pre) {
             row_sum<TPR, 1>(s, red, par);
             const float rh = 1.0f / sqrtf(s[0] * a.inv_d + a.eps);
-            columns<V, TPR>(d, t, [&](int q, int c) {
+            columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
                 float u[V];
 #pragma unroll
                 for (int e = 0; e < V; e++) u[e] = x[q + e] * rh * wq[q + e];
-                st<T, V>((T*)a.u + r * a.ldu + c, u);
+                st<T>((T*)a.u + r * a.ldu + c, n, u);
             });
         }
     }
 }
 
 // The workgroups cover the rows in runs that do not cross a gate's rows
-// (runs_per_gate of them a gate), or take gates_per_run whole gates each.
-template <typename T, int V, int TPR>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(const NormArgs a) {
-    constexpr int RL = TPR < 256 ? 256 / TPR : 1;
-    __shared__ float red[2][TPR / 64 * 3];
-    int par = 0;
+// (runs_per_gate of them a gate), or (WHOLE) take gates_per_run whole gates each.  Both
+// column sums with dX come from one: with c = sum over a gate's rows of dX yh,
+// dg = s w_post c and dw_post = s g c, added over the gates.
+template <typename T, int NV, int TPR, bool WHOLE>
+__global__ __launch_bounds__(512, NV == 8 ? 4 : 2) void norm_bwd_kernel(const NormArgs a) {
+    constexpr int V = VEC<T>;
+    constexpr int RL = 512 / TPR;
+    __shared__ float red[2][512 / 64 * 3];
     __shared__ float col[RL > 1 ? RL * NV * TPR : 1];
+    int par = 0;
     const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR, d = a.d;
-    float wp[NV], wq[NV], g[NV], s_pre[NV], s_post[NV], s_gate[NV];
+    float wq[NV], gw[NV], s_pre[NV], s_c[NV];                 // w_pre, s g w_post, sums of du hh and dX yh
 #pragma unroll
-    for (int q = 0; q < NV; q++) wp[q] = 1.0f, wq[q] = 0.0f, g[q] = s_pre[q] = s_post[q] = s_gate[q] = 0.0f;
-    columns<V, TPR>(d, t, [&](int q, int c) {
-        if (a.w_post) ldp<V>(a.w_post + c, wp + q);
-        if (a.w_pre) ldp<V>(a.w_pre + c, wq + q);
-    });
-    // a thread's column sums, added over the workgroup's rows, to dst[0 .. d)
-    auto flush = [&](const float* v, float* dst) {
+    for (int q = 0; q < NV; q++) wq[q] = gw[q] = s_pre[q] = s_c[q] = 0.0f;
+    if (a.w_pre) columns<V, NV, TPR>(d, t, [&](int q, int c, int n) { ldp<V>(a.w_pre + c, n, wq + q); });
+    // a thread's column sums, added over the workgroup's rows, as
+    // out(column, values left, sums)
+    auto flush = [&](const float* v, auto&& out) {
         if constexpr (RL > 1) {
             __syncthreads();
 #pragma unroll
             for (int q = 0; q < NV; q++) col[(rl * NV + q) * TPR + t] = v[q];
             __syncthreads();
-            if (rl == 0) {
-                columns<V, TPR>(d, t, [&](int q, int c) {
+        }
+        if (rl == 0) {
+            columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
+                float u[V];
 #pragma unroll
-                    for (int e = 0; e < V; e++) {
-                        float u = 0.0f;
+                for (int e = 0; e < V; e++) {
+                    u[e] = v[q + e];
+                    if constexpr (RL > 1) {
+                        u[e] = 0.0f;
 #pragma unroll
-                        for (int l = 0; l < RL; l++) u += col[(l * NV + q + e) * TPR + t];
-                        dst[c + e] = u;
+                        for (int l = 0; l < RL; l++) u[e] += col[(l * NV + q + e) * TPR + t];
                     }
-                });
-            }
-        } else {
-            columns<V, TPR>(d, t, [&](int q, int c) {
-#pragma unroll
-                for (int e = 0; e < V; e++) dst[c + e] = v[q + e];
+                }
+                out(c, n, u);
             });
         }
     };
     const long long bid = blockIdx.x;
     // gates [g0, g1) of gate_rows rows each; a run inside one gate takes its
     // rows [o0, o1)
-    const long long g0 = a.runs_per_gate > 1 ? bid / a.runs_per_gate : bid * a.gates_per_run;
-    const long long g1 = a.runs_per_gate > 1 ? g0 + 1 : min(g0 + a.gates_per_run, a.gates);
-    const long long o0 = a.runs_per_gate > 1 ? (bid - g0 * a.runs_per_gate) * a.run : 0;
-    const long long o1 = a.runs_per_gate > 1 ? min(o0 + a.run, a.gate_rows) : a.gate_rows;
+    const long long g0 = WHOLE ? bid * a.gates_per_run : bid / a.runs_per_gate;
+    const long long g1 = WHOLE ? min(g0 + a.gates_per_run, a.gates) : g0 + 1;
+    const long long o0 = WHOLE ? 0 : (bid - g0 * a.runs_per_gate) * a.run;
+    const long long o1 = WHOLE ? a.gate_rows : min(o0 + a.run, a.gate_rows);
     for (long long gr = g0; gr < g1; gr++) {
-        columns<V, TPR>(d, t, [&](int q, int c) {
-            float u[V];
-            if (a.gate) ldp<V>(a.gate + gr * d + c, u);
+        columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
+            float u[V], w[V];
+            if (a.gate) ldp<V>(a.gate + gr * d + c, n, u);
+            if (a.w_post) ldp<V>(a.w_post + c, n, w);
 #pragma unroll
-            for (int e = 0; e < V; e++) g[q + e] = a.gate ? a.scale * u[e] : a.scale;
+            for (int e = 0; e < V; e++) gw[q + e] = (a.gate ? a.scale * u[e] : a.scale) * (a.w_post ? w[e] : 1.0f);
         });
-        for (long long r = gr * a.gate_rows + o0 + rl; r < gr * a.gate_rows + o1; r += RL) {
+        // the workgroup's rows in step, for the barriers of their sums: where the
+        // last ones do not exist, the run's last row is computed and dropped
+        for (long long rb = o0; rb < o1; rb += RL) {
+            const bool live = rb + rl < o1;
+            const long long r = gr * a.gate_rows + (live ? rb + rl : o1 - 1);
             float x[NV], y[NV], h[NV], du[NV], s[3] = {0.0f, 0.0f, 0.0f};
-            columns<V, TPR>(d, t, [&](int q, int c) {
-                ld<T, V>((const T*)a.x + r * a.ldx + c, x + q);          // dH
-                ld<T, V>((const T*)a.y + r * a.ldy + c, y + q);
+            columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
+                ld<T>((const T*)a.x + r * a.ldx + c, n, x + q);          // dH
+                ld<T>((const T*)a.y + r * a.ldy + c, n, y + q);
                 if (a.w_pre) {
-                    ld<T, V>((const T*)a.h + r * a.ldh + c, h + q);
-                    ld<T, V>((const T*)a.u + r * a.ldu + c, du + q);     // dU
+                    ld<T>((const T*)a.h + r * a.ldh + c, n, h + q);
+                    ld<T>((const T*)a.u + r * a.ldu + c, n, du + q);     // dU
                 }
+            });
+            columns<V, NV, TPR>(d, t, [&](int q, int, int) {
 #pragma unroll
                 for (int e = 0; e < V; e++) {
                     s[0] += y[q + e] * y[q + e];
@@ -242,64 +280,100 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_bwd_kernel(const N
             const float rh = 1.0f / sqrtf(s[1] * a.inv_d + a.eps);
             const float mh = s[2] * rh * a.inv_d;                        // mean(t hh)
             float m[1] = {0.0f};
-            columns<V, TPR>(d, t, [&](int q, int c) {
+            columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
 #pragma unroll
                 for (int e = 0; e < V; e++) {
                     if (a.w_pre) {
                         const float hh = h[q + e] * rh;
                         x[q + e] += rh * (du[q + e] * wq[q + e] - hh * mh);
-                        s_pre[q + e] += du[q + e] * hh;
+                        s_pre[q + e] += live ? du[q + e] * hh : 0.0f;
                     }
-                    const float yh = y[q + e] * ry, b = g[q + e] * x[q + e];
-                    s_gate[q + e] += a.scale * x[q + e] * (yh * wp[q + e]);
-                    s_post[q + e] += b * yh;
-                    m[0] += b * wp[q + e] * yh;
+                    const float yh = y[q + e] * ry;
+                    s_c[q + e] += live ? x[q + e] * yh : 0.0f;
+                    m[0] += gw[q + e] * x[q + e] * yh;                   // b w_post yh
                     y[q + e] = yh;
                 }
-                st<T, V>((T*)a.dx + r * a.lddx + c, x + q);
+                if (live) st<T>((T*)a.dx + r * a.lddx + c, n, x + q);
             });
             float my = 0.0f;
             if (a.w_post) {
                 row_sum<TPR, 1>(m, red, par);
                 my = m[0] * a.inv_d;
             }
-            columns<V, TPR>(d, t, [&](int q, int c) {
+            columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
                 float o[V];
 #pragma unroll
-                for (int e = 0; e < V; e++) o[e] = ry * (g[q + e] * x[q + e] * wp[q + e] - y[q + e] * my);
-                st<T, V>((T*)a.dy + r * a.lddy + c, o);
+                for (int e = 0; e < V; e++) o[e] = ry * (gw[q + e] * x[q + e] - y[q + e] * my);
+                if (live) st<T>((T*)a.dy + r * a.lddy + c, n, o);
             });
         }
-        if (a.gate) {
-            flush(s_gate, a.p_gate + (a.runs_per_gate > 1 ? bid : gr) * d);
+        if constexpr (!WHOLE) {                               // the join makes both gradients of it
+            if (a.p_c) flush(s_c, [&](int c, int n, const float* u) { stp<V>(a.p_c + bid * d + c, n, u); });
+        } else if (a.gate || a.w_post) {
+            float* const pg = a.gate ? a.p_gate + gr * d : nullptr;
+            float* const pw = a.w_post ? a.p_post + bid * d : nullptr;
+            flush(s_c, [&](int c, int n, const float* u) {
+                float v[V], o[V];
+                if (pg) {
+                    if (pw) ldp<V>(a.w_post + c, n, v);
 #pragma unroll
-            for (int q = 0; q < NV; q++) s_gate[q] = 0.0f;
+                    for (int e = 0; e < V; e++) o[e] = a.scale * u[e] * (pw ? v[e] : 1.0f);
+                    stp<V>(pg + c, n, o);
+                }
+                if (pw) {
+                    if (pg) ldp<V>(a.gate + gr * d + c, n, v);
+#pragma unroll
+                    for (int e = 0; e < V; e++) o[e] = a.scale * u[e] * (pg ? v[e] : 1.0f);
+                    if (gr != g0) {                           // the gates before this one
+                        ldp<V>(pw + c, n, v);
+#pragma unroll
+                        for (int e = 0; e < V; e++) o[e] += v[e];
+                    }
+                    stp<V>(pw + c, n, o);
+                }
+            });
         }
+#pragma unroll
+        for (int q = 0; q < NV; q++) s_c[q] = 0.0f;
     }
-    if (a.w_pre) flush(s_pre, a.p_pre + bid * d);
-    if (a.w_post) flush(s_post, a.p_post + bid * d);
+    if (a.w_pre) {
+        float* const pq = a.p_pre + bid * d;
+        flush(s_pre, [&](int c, int n, const float* u) { stp<V>(pq + c, n, u); });
+    }
 }
 
-// dst[k][c] = sum of n consecutive partial rows, in a fixed order: 32 columns a
+// dst[row][c] = f[c] (sum over n consecutive partial rows k, in a fixed order,
+// of src[k][c], times mul[k / per][c] where there is one): 32 columns a
 // workgroup, 32 threads a column, each taking every 32nd row, four loads at a
 // time.
+struct JoinJob {
+    const float* src;
+    const float* mul;
+    const float* f;               // NULL: 1
+    float* dst;
+    float scale;
+    int n, rows, per;             // partial rows of a result row, result rows
+};
 struct JoinArgs {
-    const float* src[3];
-    float* dst[3];
-    int n[3], rows[3];            // partial rows of a result row, result rows
+    JoinJob job[3];
     int d;
 };
 __global__ __launch_bounds__(1024) void norm_join_kernel(const JoinArgs a) {
     __shared__ float red[32][33];
-    int job = 0, row = blockIdx.y;
-    while (row >= a.rows[job]) row -= a.rows[job++];
-    const int x = threadIdx.x & 31, l = threadIdx.x >> 5, c = blockIdx.x * 32 + x, n = a.n[job];
-    const float* p = a.src[job] + (size_t)row * n * a.d + min(c, a.d - 1);
+    int j = 0, row = blockIdx.y;
+    while (row >= a.job[j].rows) row -= a.job[j++].rows;
+    const JoinJob& o = a.job[j];
+    const int x = threadIdx.x & 31, l = threadIdx.x >> 5, c = blockIdx.x * 32 + x, cc = min(c, a.d - 1), n = o.n;
+    const float* p = o.src + (size_t)row * n * a.d + cc;
     float s = 0.0f;
     for (int k = l; k < n; k += 128) {
         float v[4];
 #pragma unroll
-        for (int q = 0; q < 4; q++) v[q] = k + 32 * q < n ? p[(size_t)(k + 32 * q) * a.d] : 0.0f;
+        for (int q = 0; q < 4; q++) {
+            const int i = k + 32 * q;
+            v[q] = i < n ? p[(size_t)i * a.d] : 0.0f;
+            if (o.mul && i < n) v[q] *= o.mul[(size_t)(i / o.per) * a.d + cc];
+        }
         s += (v[0] + v[1]) + (v[2] + v[3]);
     }
     red[l][x] = s;
@@ -307,46 +381,42 @@ __global__ __launch_bounds__(1024) void norm_join_kernel(const JoinArgs a) {
     if (l == 0) {
 #pragma unroll
         for (int k = 1; k < 32; k++) s += red[k][x];
-        if (c < a.d) a.dst[job][(size_t)row * a.d + c] = s;
+        if (c < a.d) o.dst[(size_t)row * a.d + c] = o.scale * s * (o.f ? o.f[c] : 1.0f);
     }
 }
 
-template <typename T, int V>
+template <typename T>
 void launch_rows(const NormArgs& a, bool bwd, int tpr, unsigned grid, hipStream_t s) {
-    const dim3 b(tpr < 256 ? 256 : tpr);
-    if (bwd) {
-        if (tpr == 64) norm_bwd_kernel<T, V, 64><<<grid, b, 0, s>>>(a);
-        else if (tpr == 256) norm_bwd_kernel<T, V, 256><<<grid, b, 0, s>>>(a);
-        else norm_bwd_kernel<T, V, 512><<<grid, b, 0, s>>>(a);
-    } else {
-        if (tpr == 64) norm_fwd_kernel<T, V, 64><<<grid, b, 0, s>>>(a);
-        else if (tpr == 256) norm_fwd_kernel<T, V, 256><<<grid, b, 0, s>>>(a);
-        else norm_fwd_kernel<T, V, 512><<<grid, b, 0, s>>>(a);
-    }
+    auto go = [&](auto vals, auto threads) {
+        constexpr int NV = decltype(vals)::value, TPR = decltype(threads)::value;
+        if (bwd && a.runs_per_gate > 1) norm_bwd_kernel<T, NV, TPR, false><<<grid, 512, 0, s>>>(a);
+        else if (bwd) norm_bwd_kernel<T, NV, TPR, true><<<grid, 512, 0, s>>>(a);
+        else norm_fwd_kernel<T, NV, TPR><<<grid, TPR == 64 ? 256 : TPR, 0, s>>>(a);
+    };
+    const std::integral_constant<int, 8> v8;
+    if (norm_vals(a.d) == 16) go(std::integral_constant<int, 16>{}, std::integral_constant<int, 512>{});
+    else if (tpr == 64) go(v8, std::integral_constant<int, 64>{});
+    else if (tpr == 128) go(v8, std::integral_constant<int, 128>{});
+    else if (tpr == 256) go(v8, std::integral_constant<int, 256>{});
+    else go(v8, std::integral_constant<int, 512>{});
 }
 
-int launch(const NormArgs& a, bool bwd, bool bf16, bool vec, unsigned grid, hipStream_t s) {
-    const int tpr = norm_tpr(a.d);
-    if (bf16) {
-        if (vec) launch_rows<__bf16, 8>(a, bwd, tpr, grid, s);
-        else launch_rows<__bf16, 1>(a, bwd, tpr, grid, s);
-    } else {
-        if (vec) launch_rows<float, 4>(a, bwd, tpr, grid, s);
-        else launch_rows<float, 1>(a, bwd, tpr, grid, s);
-    }
+int launch(const NormArgs& a, bool bwd, bool bf16, unsigned grid, hipStream_t s) {
+    if (bf16) launch_rows<__bf16>(a, bwd, norm_tpr(a.d), grid, s);
+    else launch_rows<float>(a, bwd, norm_tpr(a.d), grid, s);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_HIP;
 }
 
-// Runs of the backward pass: about NORM_RUNS workgroups, none crossing a gate.
+// Runs of the backward pass: about norm_runs() workgroups, none crossing a gate.
 void plan_runs(NormArgs& a) {
-    const long long rl = norm_tpr(a.d) < 256 ? 256 / norm_tpr(a.d) : 1;
-    if (a.gates >= NORM_RUNS) {
+    const long long rl = norm_bwd_rows(a.d);
+    if (a.gates >= norm_runs(a.d)) {
         a.runs_per_gate = 1;
-        a.gates_per_run = (a.gates + NORM_RUNS - 1) / NORM_RUNS;
+        a.gates_per_run = (a.gates + norm_runs(a.d) - 1) / norm_runs(a.d);
         a.run = a.gate_rows;
         a.runs = (a.gates + a.gates_per_run - 1) / a.gates_per_run;
     } else {
-        const long long want = std::max<long long>(1, NORM_RUNS / a.gates);
+        const long long want = std::max<long long>(1, norm_runs(a.d) / a.gates);
         a.run = std::max<long long>(rl, (a.gate_rows + want - 1) / want);
         a.runs_per_gate = (a.gate_rows + a.run - 1) / a.run;
         a.gates_per_run = 1;
@@ -356,22 +426,26 @@ void plan_runs(NormArgs& a) {
 
 }  // namespace
 
-int launch_norm_fwd(NormArgs a, bool bf16, bool vec, hipStream_t s) {
-    const long long rl = norm_tpr(a.d) < 256 ? 256 / norm_tpr(a.d) : 1;
+int launch_norm_fwd(NormArgs a, bool bf16, hipStream_t s) {
+    const long long rl = norm_fwd_rows(a.d);
     a.run = std::max<long long>(rl, (a.rows + NORM_FWD_RUNS - 1) / NORM_FWD_RUNS);
-    return launch(a, false, bf16, vec, (unsigned)((a.rows + a.run - 1) / a.run), s);
+    return launch(a, false, bf16, (unsigned)((a.rows + a.run - 1) / a.run), s);
+}
+
+// Partial arrays of the backward pass: du hh's, and dX yh's or dw_post's.
+static int norm_parts(const NormArgs& a, bool gate, bool post, bool pre) {
+    const bool c = a.runs_per_gate > 1 ? gate || post : post;
+    return (pre ? 1 : 0) + (c ? 1 : 0);
 }
 
 size_t norm_bwd_workspace(long long rows, int d, long long gates, bool gate, bool post, bool pre) {
     NormArgs a;
     a.d = d; a.rows = rows; a.gates = gates; a.gate_rows = rows / gates;
     plan_runs(a);
-    const long long n = (post ? a.runs : 0) + (pre ? a.runs : 0) + (gate && a.runs_per_gate > 1 ? a.runs : 0);
-    return a.runs == 1 ? 0 : (size_t)n * d * sizeof(float);
+    return a.runs == 1 ? 0 : (size_t)norm_parts(a, gate, post, pre) * a.runs * d * sizeof(float);
 }
 
-int launch_norm_bwd(NormArgs a, bool bf16, bool vec, float* dw_pre, float* dw_post, float* dgate, void* ws,
-                    hipStream_t s) {
+int launch_norm_bwd(NormArgs a, bool bf16, float* dw_pre, float* dw_post, float* dgate, void* ws, hipStream_t s) {
     plan_runs(a);
     const bool one = a.runs == 1;                 // a single workgroup writes the results itself
     float* p = (float*)ws;
@@ -382,24 +456,27 @@ int launch_norm_bwd(NormArgs a, bool bf16, bool vec, float* dw_pre, float* dw_po
         return q;
     };
     a.p_pre = a.w_pre ? take(dw_pre) : nullptr;
-    a.p_post = a.w_post ? take(dw_post) : nullptr;
-    a.p_gate = a.gate ? (a.runs_per_gate > 1 ? take(dgate) : dgate) : nullptr;
-    int rc = launch(a, true, bf16, vec, (unsigned)a.runs, s);
+    const bool c = a.runs_per_gate > 1 && (a.gate || a.w_post);
+    a.p_c = c ? take(nullptr) : nullptr;
+    a.p_post = !c && a.w_post ? take(dw_post) : nullptr;
+    a.p_gate = !c ? dgate : nullptr;
+    int rc = launch(a, true, bf16, (unsigned)a.runs, s);
     if (rc || one) return rc;
-    JoinArgs j;
-    int nj = 0, nrows = 0;
-    auto add = [&](const float* src, float* dst, long long n, long long rows) {
-        j.src[nj] = src; j.dst[nj] = dst; j.n[nj] = (int)n; j.rows[nj] = (int)rows;
-        nj++;
-        nrows += (int)rows;
+    JoinArgs j = {};
+    int nj = 0;
+    long long nrows = 0;
+    auto add = [&](JoinJob job) {
+        j.job[nj++] = job;
+        nrows += job.rows;
     };
-    if (a.w_pre) add(a.p_pre, dw_pre, a.runs, 1);
-    if (a.w_post) add(a.p_post, dw_post, a.runs, 1);
-    if (a.gate && a.runs_per_gate > 1) add(a.p_gate, dgate, a.runs_per_gate, a.gates);
+    const int runs = (int)a.runs, per = (int)a.runs_per_gate;
+    if (a.w_pre) add({a.p_pre, nullptr, nullptr, dw_pre, 1.0f, runs, 1, 1});
+    if (c && a.gate) add({a.p_c, nullptr, a.w_post, dgate, a.scale, per, (int)a.gates, 1});
+    if (c && a.w_post) add({a.p_c, a.gate, nullptr, dw_post, a.scale, runs, 1, per});
+    if (a.p_post) add({a.p_post, nullptr, nullptr, dw_post, 1.0f, runs, 1, 1});
     if (!nj) return MXC_OK;
-    for (int k = nj; k < 3; k++) { j.src[k] = j.src[0]; j.dst[k] = j.dst[0]; j.n[k] = j.rows[k] = 0; }
     j.d = a.d;
-    norm_join_kernel<<<dim3((a.d + 31) / 32, nrows), 1024, 0, s>>>(j);
+    norm_join_kernel<<<dim3((a.d + 31) / 32, (unsigned)nrows), 1024, 0, s>>>(j);
     return hipGetLastError() == hipSuccess ? MXC_OK : MXC_ERR_HIP;
 }
 
