@@ -11,6 +11,8 @@ struct LinPlan {
     long long ldw;                // row length of the partial sums
 };
 
+constexpr int LIN_SPLIT_UNITS = 16;
+
 // nra, nrb: 32-blocks along the output's columns and rows; ncb: along the
 // contraction.  The formats play no part, so neither do they in the workspace.
 LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
@@ -23,12 +25,12 @@ LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
     else { q.tile = LIN_TILE_64; q.ra = 2; q.rb = 2; }
     q.ta = (nra + q.ra - 1) / q.ra;
     q.tb = (nrb + q.rb - 1) / q.rb;
-    // a grid that leaves CUs idle is split along the contraction, in units of
-    // 16 blocks (a whole number of any shape's stages), two of them a split at
-    // least, four where a stage is a whole unit
+    // a grid that leaves CUs idle is split along a long contraction, in units of
+    // 16 blocks (a whole number of any shape's stages), four of them a split at
+    // least
     const long long t = (long long)q.ta * q.tb;
     const int units = (ncb + 15) / 16;
-    const int n = t < 256 ? std::max(1, (int)std::min<long long>(256 / t, units / (q.tile <= LIN_TILE_ROWS64 ? 4 : 2))) : 1;
+    const int n = t < 256 && units >= LIN_SPLIT_UNITS ? std::max(1, (int)std::min<long long>(256 / t, units / 4)) : 1;
     q.span = (units + n - 1) / n * 16;
     q.nsplit = (ncb + q.span - 1) / q.span;
     q.ldw = (long long)nra * 32;

@@ -36,15 +36,14 @@ struct LinOp {
 // The epilogue: out[r][c] for output row r < nrows, column c < ncols.
 //   fwd    z = v + bias[c]; pre[r][c] = z; out = fn(z) + res[r][c]
 //   dgrad  out = v fn'(z[r][c]) + res[r][c]
-// pre doubles as dgrad's z.  vec: 1 where ncols and every stride allow vectors
-// of four columns, 2 where they allow 16 bytes.
+// pre doubles as dgrad's z.
 struct LinEpi {
     void* out;
     const float* bias;
     const void* res;
     void* pre;
     long long ldo, ldr, ldp;
-    int fn, bf16, vec;
+    int fn, bf16;
     int nrows, ncols;
 };
 
@@ -138,103 +137,108 @@ __device__ __forceinline__ float lin_value(int fn, float v, float b, float z, fl
     }
 }
 
-template <bool BF>
-__device__ __forceinline__ float4 lin_load4(const void* p, long long i) {
-    if constexpr (BF) return bf16_unpack4(*(const uint2*)((const uint16_t*)p + i));
-    else return *(const float4*)((const float*)p + i);
-}
-template <bool BF>
-__device__ __forceinline__ void lin_store4(void* p, long long i, float4 v) {
-    if constexpr (BF) *(uint2*)((uint16_t*)p + i) = bf16_pack4(v.x, v.y, v.z, v.w);
-    else *(float4*)((float*)p + i) = v;
-}
-__device__ __forceinline__ float lin_load1(const void* p, long long i, int bf16) {
-    return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[i] << 16) : ((const float*)p)[i];
-}
-__device__ __forceinline__ void lin_store1(void* p, long long i, int bf16, float v) {
-    if (bf16) ((uint16_t*)p)[i] = (uint16_t)bf16_bits(v);
-    else ((float*)p)[i] = v;
-}
-
-// Four consecutive columns c .. c + 3 of output row r, c + 3 < ncols, r <
-// nrows, as vectors (e.vec): what they read, and their results.  All
-// arithmetic is fp32, rounded once where it is stored; the activation is
-// applied to the unrounded pre-activation.
-struct LinAux {
-    float4 z, s;
+// N consecutive values of a full-precision row, of which `left` are before the
+// row's end: one access of N elements at any element's address (global memory
+// takes unaligned vectors), or element by element where the row ends inside.
+template <int BYTES, int AL> struct __attribute__((packed, aligned(AL))) LinRaw {
+    uint32_t w[BYTES / 4];
 };
-template <int OP, bool BF>
-__device__ __forceinline__ LinAux lin_read4(const LinEpi& e, int r, int c) {
-    LinAux a;
-    a.z = a.s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (OP == LIN_FWD && e.bias) a.z = *(const float4*)(e.bias + c);
-    if (OP == LIN_DGRAD && e.fn != MXC_FN_NONE) a.z = lin_load4<BF>(e.pre, r * e.ldp + c);
-    if (OP != LIN_WGRAD && e.res) a.s = lin_load4<BF>(e.res, r * e.ldr + c);
-    return a;
-}
-template <int OP, bool BF>
-__device__ __forceinline__ void lin_write4(const LinEpi& e, int r, int c, float4 v, const LinAux& a) {
-    const float4 z = a.z, s = a.s;
-    if (OP == LIN_FWD && e.pre)
-        lin_store4<BF>(e.pre, r * e.ldp + c, make_float4(v.x + z.x, v.y + z.y, v.z + z.z, v.w + z.w));
-    // one uniform choice of the activation around four independent values
-    auto four = [&](int fn) {
-        lin_store4<BF>(e.out, r * e.ldo + c,
-                       make_float4(lin_value<OP>(fn, v.x, z.x, z.x, s.x), lin_value<OP>(fn, v.y, z.y, z.y, s.y),
-                                   lin_value<OP>(fn, v.z, z.z, z.z, s.z), lin_value<OP>(fn, v.w, z.w, z.w, s.w)));
-    };
-    if (OP == LIN_WGRAD || e.fn == MXC_FN_NONE) four(MXC_FN_NONE);
-    else if (e.fn == MXC_FN_RELU) four(MXC_FN_RELU);
-    else four(MXC_FN_SILU);
-}
-
-// Any alignment, column by column; columns past ncols are dropped.
-template <int OP>
-__device__ __forceinline__ void lin_scalar4(const LinEpi& e, int r, int c, float4 v) {
-    const float a[4] = {v.x, v.y, v.z, v.w};
+template <bool BF, int N>
+__device__ __forceinline__ void lin_load(const void* base, long long i, int left, float* o) {
+    if constexpr (BF) {
+        const uint16_t* p = (const uint16_t*)base + i;
+        if (left >= N) {
+            const LinRaw<2 * N, 2> u = *(const LinRaw<2 * N, 2>*)p;
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
-        if (c + q >= e.ncols) return;
-        const float b = OP == LIN_FWD && e.bias ? e.bias[c + q] : 0.0f;
-        const float z = OP == LIN_DGRAD && e.fn != MXC_FN_NONE ? lin_load1(e.pre, r * e.ldp + c + q, e.bf16) : 0.0f;
-        const float s = OP != LIN_WGRAD && e.res ? lin_load1(e.res, r * e.ldr + c + q, e.bf16) : 0.0f;
-        if (OP == LIN_FWD && e.pre) lin_store1(e.pre, r * e.ldp + c + q, e.bf16, a[q] + b);
-        lin_store1(e.out, r * e.ldo + c + q, e.bf16, lin_value<OP>(e.fn, a[q], b, z, s));
-    }
-}
-
-template <int OP>
-__device__ __forceinline__ void lin_epilogue4(const LinEpi& e, int r, int c, float4 v) {
-    if (!e.vec) lin_scalar4<OP>(e, r, c, v);
-    else if (c >= e.ncols) return;
-    else if (e.bf16) lin_write4<OP, true>(e, r, c, v, lin_read4<OP, true>(e, r, c));
-    else lin_write4<OP, false>(e, r, c, v, lin_read4<OP, false>(e, r, c));
-}
-
-// 16 bytes of a full-precision row: 8 bf16 or 4 fp32 columns.
-template <bool BF> constexpr int LIN_V = BF ? 8 : 4;
-template <bool BF>
-__device__ __forceinline__ void lin_unpack(uint4 u, float* o) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int k = 0; k < 4; k++) {
-        if constexpr (BF) {
-            o[2 * k] = __uint_as_float(w[k] << 16);
-            o[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+            for (int k = 0; k < N / 2; k++) {
+                o[2 * k] = __uint_as_float(u.w[k] << 16);
+                o[2 * k + 1] = __uint_as_float(u.w[k] & 0xFFFF0000u);
+            }
         } else {
-            o[k] = __uint_as_float(w[k]);
+#pragma unroll
+            for (int k = 0; k < N; k++) o[k] = k < left ? __uint_as_float((uint32_t)p[k] << 16) : 0.0f;
+        }
+    } else {
+        const float* p = (const float*)base + i;
+        if (left >= N) {
+            const LinRaw<4 * N, 4> u = *(const LinRaw<4 * N, 4>*)p;
+#pragma unroll
+            for (int k = 0; k < N; k++) o[k] = __uint_as_float(u.w[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k++) o[k] = k < left ? p[k] : 0.0f;
         }
     }
 }
-template <bool BF>
-__device__ __forceinline__ void lin_put(void* p, long long i, const float* v) {
-    if constexpr (BF) *(uint4*)((uint16_t*)p + i) = make_uint4(bf16_pack2(v[0], v[1]), bf16_pack2(v[2], v[3]),
-                                                               bf16_pack2(v[4], v[5]), bf16_pack2(v[6], v[7]));
-    else *(float4*)((float*)p + i) = make_float4(v[0], v[1], v[2], v[3]);
+template <bool BF, int N>
+__device__ __forceinline__ void lin_store(void* base, long long i, int left, const float* v) {
+    if constexpr (BF) {
+        uint16_t* p = (uint16_t*)base + i;
+        if (left >= N) {
+            LinRaw<2 * N, 2> u;
+#pragma unroll
+            for (int k = 0; k < N / 2; k++) u.w[k] = bf16_pack2(v[2 * k], v[2 * k + 1]);
+            *(LinRaw<2 * N, 2>*)p = u;
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k++)
+                if (k < left) p[k] = (uint16_t)bf16_bits(v[k]);
+        }
+    } else {
+        float* p = (float*)base + i;
+        if (left >= N) {
+            LinRaw<4 * N, 4> u;
+#pragma unroll
+            for (int k = 0; k < N; k++) u.w[k] = __float_as_uint(v[k]);
+            *(LinRaw<4 * N, 4>*)p = u;
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; k++)
+                if (k < left) p[k] = v[k];
+        }
+    }
 }
-template <bool BF>
-__device__ __forceinline__ uint4 lin_get(const void* p, long long i) {
-    return BF ? *(const uint4*)((const uint16_t*)p + i) : *(const uint4*)((const float*)p + i);
+
+// N consecutive columns c .. of output row r < nrows (those before ncols): the
+// values v with what the epilogue reads (z: the pre-activation, s: the
+// residual).  All arithmetic is fp32, rounded once where it is stored; the
+// activation is applied to the unrounded pre-activation.
+template <int OP, bool BF, int N, int FN>
+__device__ __forceinline__ void lin_finish(const LinEpi& e, int r, int c, float* v, const float* b, float* z, const float* s) {
+    const int left = e.ncols - c;
+    if (OP == LIN_FWD && e.pre) {
+#pragma unroll
+        for (int q = 0; q < N; q++) z[q] = v[q] + b[q];
+        lin_store<BF, N>(e.pre, r * e.ldp + c, left, z);
+    }
+#pragma unroll
+    for (int q = 0; q < N; q++) v[q] = lin_value<OP>(FN, v[q], b[q], z[q], s[q]);
+    lin_store<BF, N>(e.out, r * e.ldo + c, left, v);
+}
+
+// body(FnTag) for the epilogue's activation, one uniform choice
+template <int OP, class Body>
+__device__ __forceinline__ void lin_fn(const LinEpi& e, Body&& body) {
+    if (OP == LIN_WGRAD || e.fn == MXC_FN_NONE) body(FnTag<MXC_FN_NONE>{});
+    else if (e.fn == MXC_FN_RELU) body(FnTag<MXC_FN_RELU>{});
+    else body(FnTag<MXC_FN_SILU>{});
+}
+
+// Four columns, where they come one by one (split sums, joined waves).
+template <int OP, bool BF>
+__device__ __forceinline__ void lin_four(const LinEpi& e, int r, int c, float4 v) {
+    const int left = e.ncols - c;
+    if (left <= 0) return;
+    float a[4] = {v.x, v.y, v.z, v.w}, b[4] = {0, 0, 0, 0}, z[4] = {0, 0, 0, 0}, s[4] = {0, 0, 0, 0};
+    if (OP == LIN_FWD && e.bias) lin_load<false, 4>(e.bias, c, left, b);
+    if (OP == LIN_DGRAD && e.fn != MXC_FN_NONE) lin_load<BF, 4>(e.pre, r * e.ldp + c, left, z);
+    if (OP != LIN_WGRAD && e.res) lin_load<BF, 4>(e.res, r * e.ldr + c, left, s);
+    lin_fn<OP>(e, [&](auto fn) { lin_finish<OP, BF, 4, decltype(fn)::fn>(e, r, c, a, b, z, s); });
+}
+template <int OP>
+__device__ __forceinline__ void lin_epilogue4(const LinEpi& e, int r, int c, float4 v) {
+    if (OP != LIN_WGRAD && e.bf16) lin_four<OP, true>(e, r, c, v);
+    else lin_four<OP, false>(e, r, c, v);
 }
 
 // One 32-row block of a wave (rows r0 .. r0 + 31, columns c0 .. c0 + 32 MB -
@@ -243,65 +247,50 @@ __device__ __forceinline__ uint4 lin_get(const void* p, long long i) {
 // park() writes the block to LDS; the first batch's reads are issued before it.
 template <int OP, bool BF, int MB, class Park>
 __device__ __forceinline__ void lin_rows(const LinEpi& e, int r0, int c0, const float* mine, int lane, Park&& park) {
-    constexpr int V = LIN_V<BF>, LD = 32 * MB + 4;
+    constexpr int V = BF ? 8 : 4, LD = 32 * MB + 4;
     constexpr int LPR = 32 * MB / V, RS = 64 / LPR, CNT = 32 / RS, BN = CNT < 4 ? CNT : 4;
-    const int row = lane / LPR, col = lane % LPR * V, c = c0 + col, cc = c < e.ncols ? c : 0;
+    const int row = lane / LPR, col = lane % LPR * V, c = c0 + col;
+    // a lane past the last column reads the row's first ones and stores nothing
+    const int cc = c < e.ncols ? c : 0, left = e.ncols - cc;
     const bool rd_z = OP == LIN_DGRAD && e.fn != MXC_FN_NONE, rd_s = OP != LIN_WGRAD && e.res;
-    uint4 z[BN], s[BN];
+    float z[BN][V], s[BN][V], b[V];
+#pragma unroll
+    for (int k = 0; k < BN; k++)
+#pragma unroll
+        for (int q = 0; q < V; q++) z[k][q] = s[k][q] = 0.0f;
+#pragma unroll
+    for (int q = 0; q < V; q++) b[q] = 0.0f;
     auto read = [&](int n) {
 #pragma unroll
         for (int k = 0; k < BN; k++) {
             const int r = min(r0 + row + (n + k) * RS, e.nrows - 1);
-            if (rd_z) z[k] = lin_get<BF>(e.pre, r * e.ldp + cc);
-            if (rd_s) s[k] = lin_get<BF>(e.res, r * e.ldr + cc);
+            if (rd_z) lin_load<BF, V>(e.pre, r * e.ldp + cc, left, z[k]);
+            if (rd_s) lin_load<BF, V>(e.res, r * e.ldr + cc, left, s[k]);
         }
     };
     read(0);
-    float b[V];
-#pragma unroll
-    for (int k = 0; k < V; k++) b[k] = 0.0f;
     if (OP == LIN_FWD && e.bias) {
-#pragma unroll
-        for (int k = 0; k < V; k += 4) {
-            const float4 u = *(const float4*)(e.bias + cc + k);
-            b[k] = u.x; b[k + 1] = u.y; b[k + 2] = u.z; b[k + 3] = u.w;
-        }
+        lin_load<false, 4>(e.bias, cc, left, b);
+        if constexpr (V == 8) lin_load<false, 4>(e.bias, left > 4 ? cc + 4 : cc, left - 4, b + 4);
     }
     park();
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
     for (int n = 0; n < CNT; n += BN) {
         if (n) read(n);
-        auto rows = [&](auto fn) {
-            constexpr int FN = decltype(fn)::fn;
+        lin_fn<OP>(e, [&](auto fn) {
 #pragma unroll
             for (int k = 0; k < BN; k++) {
                 const int r = r0 + row + (n + k) * RS;
-                float v[V], zf[V], sf[V];
+                float v[V];
 #pragma unroll
                 for (int q = 0; q < V; q += 4) {
                     const float4 u = *(const float4*)(mine + (row + (n + k) * RS) * LD + col + q);
                     v[q] = u.x; v[q + 1] = u.y; v[q + 2] = u.z; v[q + 3] = u.w;
                 }
-#pragma unroll
-                for (int q = 0; q < V; q++) zf[q] = sf[q] = 0.0f;
-                if (FN != MXC_FN_NONE && OP == LIN_DGRAD) lin_unpack<BF>(z[k], zf);
-                if (rd_s) lin_unpack<BF>(s[k], sf);
-                if (r < e.nrows && c < e.ncols) {
-                    if (OP == LIN_FWD && e.pre) {
-#pragma unroll
-                        for (int q = 0; q < V; q++) zf[q] = v[q] + b[q];
-                        lin_put<BF>(e.pre, r * e.ldp + c, zf);
-                    }
-#pragma unroll
-                    for (int q = 0; q < V; q++) v[q] = lin_value<OP>(FN, v[q], b[q], zf[q], sf[q]);
-                    lin_put<BF>(e.out, r * e.ldo + c, v);
-                }
+                if (r < e.nrows && c < e.ncols) lin_finish<OP, BF, V, decltype(fn)::fn>(e, r, c, v, b, z[k], s[k]);
             }
-        };
-        if (OP == LIN_WGRAD || e.fn == MXC_FN_NONE) rows(FnTag<MXC_FN_NONE>{});
-        else if (e.fn == MXC_FN_RELU) rows(FnTag<MXC_FN_RELU>{});
-        else rows(FnTag<MXC_FN_SILU>{});
+        });
     }
     __builtin_amdgcn_wave_barrier();
 }
@@ -666,7 +655,7 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
                             acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
             };
             const int r0 = (rb0 + wn * NB + j) * 32, c0 = (ra0 + wm * MB) * 32;
-            if (p.part || p.e.vec < 2) {
+            if (p.part) {
                 park();
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
@@ -675,7 +664,7 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
                     put(r0 + row, c0 + col, *(const float4*)(mine + row * LD + col));
                 }
                 __builtin_amdgcn_wave_barrier();
-            } else if (p.e.bf16) {
+            } else if (OP != LIN_WGRAD && p.e.bf16) {
                 lin_rows<OP, true, MB>(p.e, r0, c0, mine, lane, park);
             } else {
                 lin_rows<OP, false, MB>(p.e, r0, c0, mine, lane, park);

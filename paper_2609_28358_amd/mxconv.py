@@ -5,7 +5,6 @@ caller's device, pointers and the current HIP stream are passed through, and
 every step runs in the library's HIP kernels.  A missing library raises; there
 is no fallback path.
 """
-import contextlib
 import ctypes
 import functools
 import os
@@ -590,11 +589,11 @@ def quantize_sum(terms, shape, fmt, fn=FN_NONE, z=None, out=None, vals=None, str
 # run with the tensors' device current, and allocate on the stream they launch
 # on: a workspace freed at return is reused only by later work of that stream.
 LINEAR_FWD, LINEAR_DGRAD, LINEAR_WGRAD = 0, 1, 2
-_here = contextlib.nullcontext()
 
 
 def _place(device, stream):
-    """The context of a call: the device, and the stream where one is given."""
+    """The context of a call -- the stream where one is given, else the tensors'
+    device where it is not the current one -- or None."""
     if device.type != "cuda":
         raise MxconvError(f"tensors must be on a GPU, got {device}")
     if stream is not None:
@@ -602,50 +601,76 @@ def _place(device, stream):
             raise MxconvError(f"the stream is on {stream.device}, the tensors on {device}")
         return torch.cuda.stream(stream)
     here = _raw_device() if _raw_device is not None else torch.cuda.current_device()
-    return _here if device.index == here else torch.cuda.device(device)
+    return None if device.index == here else torch.cuda.device(device)
 
 
-def _rows_cols(t, what, rows, cols, dtype, device):
+def _placed(fn):
+    """Run a call's launching part, fn(..., device, stream), in its context."""
+    @functools.wraps(fn)
+    def run(*args):
+        place = _place(args[-2], args[-1])
+        if place is None:
+            return fn(*args)
+        with place:
+            return fn(*args)
+    return run
+
+
+def _rows_cols(t, what, shape, dtype, device):
     """The row stride of a row-major full-precision matrix argument."""
-    if t is None:
-        return 0
     if t.dtype != dtype:
         raise MxconvError(f"{what} must be {dtype}, got {t.dtype}")
-    if t.shape != (rows, cols):
-        raise MxconvError(f"{what} must be {rows} x {cols}, got {tuple(t.shape)}")
+    if t.shape != shape:
+        raise MxconvError(f"{what} must be {shape[0]} x {shape[1]}, got {tuple(t.shape)}")
     if t.device != device:
         raise MxconvError(f"{what} must be on {device}, got {t.device}")
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
         raise MxconvError(f"{what} must have unit column stride")
-    return t.stride(0) if rows > 1 else cols
+    return ld if shape[0] > 1 else shape[1]
 
 
 def _vector(t, what, shape, device):
     """An fp32 parameter argument."""
-    if t is None:
-        return
     if t.dtype != torch.float32 or t.shape != shape or t.device != device or not t.is_contiguous():
         raise MxconvError(f"{what} must be a contiguous fp32 tensor of shape {tuple(shape)} on {device}")
 
 
+@functools.lru_cache(maxsize=_CACHED)
+def _mx_geometry(role, fmt, shape):
+    """(rows, columns, code bytes, scale bytes) of an MX matrix, or None."""
+    r, c, h, w = shape
+    if h != 1 or w != 1 or (role == ACT and r % 32) or not codes_bytes(WEIGHT, fmt, r, c, 1, 1):
+        return None
+    return r, c, codes_bytes(WEIGHT, fmt, r, c, 1, 1), scales_bytes(WEIGHT, fmt, r, c, 1, 1)
+
+
 def _mx_matrix(q, what):
-    """(rows, columns) of an MX matrix argument: shape (R, C, 1, 1) with 32-row
-    blocks."""
-    r, c, h, w = q.shape
-    if h != 1 or w != 1 or (q.role == ACT and r % 32):
+    """(rows, columns, device) of an MX matrix argument: shape (R, C, 1, 1) with
+    32-row blocks."""
+    g = _mx_geometry(q.role, q.fmt, q.shape)
+    if g is None:
         raise MxconvError(f"{what} must be an MX matrix: shape (R, C, 1, 1), role WEIGHT (or ACT with R a multiple of 32)")
-    if (q.codes.dtype != torch.uint8 or q.scales.dtype != torch.uint8 or not q.codes.is_contiguous() or
-            not q.scales.is_contiguous() or q.codes.numel() < codes_bytes(WEIGHT, q.fmt, r, c, 1, 1) or
-            q.scales.numel() < scales_bytes(WEIGHT, q.fmt, r, c, 1, 1) or q.scales.device != q.codes.device):
+    c, s = q.codes, q.scales
+    dev = c.device
+    if (c.dtype != torch.uint8 or s.dtype != torch.uint8 or c.numel() < g[2] or s.numel() < g[3] or
+            not c.is_contiguous() or not s.is_contiguous() or s.device != dev):
         raise MxconvError(f"{what}: codes and scales must be contiguous uint8 tensors of the matrix's size on one device")
-    return r, c
+    return g[0], g[1], dev
 
 
 @functools.lru_cache(maxsize=_CACHED)
 def _linear_of(rows, outs, ins):
     """The layer's struct (only read by the library) and its workspace sizes."""
     s = MxcLinear(rows, outs, ins)
-    return s, tuple(lib().mxconv_linear_workspace_bytes(op, ctypes.byref(s)) for op in range(3))
+    return ctypes.byref(s), tuple(lib().mxconv_linear_workspace_bytes(op, ctypes.byref(s)) for op in range(3))
+
+
+def _dtype_code(dtype):
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise MxconvError(f"unsupported dtype {dtype}")
+    return code
 
 
 def linear_workspace_bytes(op, rows, outs, ins):
@@ -655,10 +680,13 @@ def linear_workspace_bytes(op, rows, outs, ins):
 def _workspace(ws, need, device):
     """(tensor to keep, pointer, bytes) of a call's workspace."""
     if ws is None:
-        ws = torch.empty(need, dtype=torch.uint8, device=device) if need else None
-    elif ws.device != device or not ws.is_contiguous():
+        if not need:
+            return None, None, 0
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        return ws, ws.data_ptr(), need
+    if ws.device != device or not ws.is_contiguous():
         raise MxconvError(f"the workspace must be a contiguous tensor on {device}")
-    return ws, _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def quantize_matrix(m, fmt, out=None, stream=None):
@@ -675,45 +703,50 @@ def linear(w, x, bias=None, fn=FN_NONE, residual=None, dtype=torch.bfloat16, out
     """Y = fn(X W^T + bias) + residual, [rows][outs] of `dtype`, from the MX
     matrices W [outs][ins] and X [rows][ins] (mxconv_linear_fwd).  pre_out
     receives X W^T + bias."""
-    (outs, ins), (rows, k), dev = _mx_matrix(w, "w"), _mx_matrix(x, "x"), x.codes.device
-    if k != ins or w.codes.device != dev:
-        raise MxconvError(f"w is {outs} x {ins} on {w.codes.device}, x {rows} x {k} on {dev}")
-    code = _DTYPES.get(dtype)
-    if code is None:
-        raise MxconvError(f"unsupported dtype {dtype}")
-    _vector(bias, "bias", (outs,), dev)
-    ldr = _rows_cols(residual, "residual", rows, outs, dtype, dev)
-    ldz = _rows_cols(pre_out, "pre_out", rows, outs, dtype, dev)
-    s, need = _linear_of(rows, outs, ins)
-    with _place(dev, stream):
-        y = out if out is not None else torch.empty((rows, outs), dtype=dtype, device=dev)
-        ldy = _rows_cols(y, "the output", rows, outs, dtype, dev)
-        ws, wp, wb = _workspace(workspace, need[0], dev)
-        _check(lib().mxconv_linear_fwd(ctypes.byref(s), pair(w.fmt, x.fmt), _ptr(w.codes), _ptr(w.scales), _ptr(x.codes),
-                                       _ptr(x.scales), _ptr(bias), fn, _ptr(residual), ldr, _ptr(y), ldy, _ptr(pre_out),
-                                       ldz, code, wp, wb, _stream(stream)), "mxconv_linear_fwd")
+    (outs, ins, wdev), (rows, k, dev) = _mx_matrix(w, "w"), _mx_matrix(x, "x")
+    if k != ins or wdev != dev:
+        raise MxconvError(f"w is {outs} x {ins} on {wdev}, x {rows} x {k} on {dev}")
+    if bias is not None:
+        _vector(bias, "bias", (outs,), dev)
+    return _linear((rows, outs), ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace, dev, stream)
+
+
+@_placed
+def _linear(shape, ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace, dev, stream):
+    code = _dtype_code(dtype)
+    y = out if out is not None else torch.empty(shape, dtype=dtype, device=dev)
+    ldr = _rows_cols(residual, "residual", shape, dtype, dev) if residual is not None else 0
+    ldz = _rows_cols(pre_out, "pre_out", shape, dtype, dev) if pre_out is not None else 0
+    ldy = _rows_cols(y, "the output", shape, dtype, dev) if out is not None else shape[1]
+    s, need = _linear_of(shape[0], shape[1], ins)
+    ws, wp, wb = _workspace(workspace, need[0], dev)
+    _check(lib().mxconv_linear_fwd(s, pair(w.fmt, x.fmt), w.codes.data_ptr(), w.scales.data_ptr(), x.codes.data_ptr(),
+                                   x.scales.data_ptr(), _ptr(bias), fn, _ptr(residual), ldr, y.data_ptr(), ldy,
+                                   _ptr(pre_out), ldz, code, wp, wb, _stream(stream)), "mxconv_linear_fwd")
     return y
 
 
 def linear_dgrad(w, dz, fn=FN_NONE, z=None, add=None, dtype=torch.bfloat16, out=None, workspace=None, stream=None):
     """dX = fn'(z) . (dZ W) + add, [rows][ins] of `dtype`, from the MX matrices
     W [outs][ins] and dZ [rows][outs] (mxconv_linear_dgrad)."""
-    (outs, ins), (rows, n), dev = _mx_matrix(w, "w"), _mx_matrix(dz, "dz"), dz.codes.device
-    if n != outs or w.codes.device != dev:
-        raise MxconvError(f"w is {outs} x {ins} on {w.codes.device}, dz {rows} x {n} on {dev}")
-    code = _DTYPES.get(dtype)
-    if code is None:
-        raise MxconvError(f"unsupported dtype {dtype}")
-    ldz = _rows_cols(z, "z", rows, ins, dtype, dev)
-    lda = _rows_cols(add, "add", rows, ins, dtype, dev)
-    s, need = _linear_of(rows, outs, ins)
-    with _place(dev, stream):
-        dx = out if out is not None else torch.empty((rows, ins), dtype=dtype, device=dev)
-        ldx = _rows_cols(dx, "the output", rows, ins, dtype, dev)
-        ws, wp, wb = _workspace(workspace, need[1], dev)
-        _check(lib().mxconv_linear_dgrad(ctypes.byref(s), pair(w.fmt, dz.fmt), _ptr(w.codes), _ptr(w.scales),
-                                         _ptr(dz.codes), _ptr(dz.scales), fn, _ptr(z), ldz, _ptr(add), lda, _ptr(dx), ldx,
-                                         code, wp, wb, _stream(stream)), "mxconv_linear_dgrad")
+    (outs, ins, wdev), (rows, n, dev) = _mx_matrix(w, "w"), _mx_matrix(dz, "dz")
+    if n != outs or wdev != dev:
+        raise MxconvError(f"w is {outs} x {ins} on {wdev}, dz {rows} x {n} on {dev}")
+    return _linear_dgrad((rows, ins), outs, w, dz, fn, z, add, dtype, out, workspace, dev, stream)
+
+
+@_placed
+def _linear_dgrad(shape, outs, w, dz, fn, z, add, dtype, out, workspace, dev, stream):
+    code = _dtype_code(dtype)
+    dx = out if out is not None else torch.empty(shape, dtype=dtype, device=dev)
+    ldz = _rows_cols(z, "z", shape, dtype, dev) if z is not None else 0
+    lda = _rows_cols(add, "add", shape, dtype, dev) if add is not None else 0
+    ldx = _rows_cols(dx, "the output", shape, dtype, dev) if out is not None else shape[1]
+    s, need = _linear_of(shape[0], outs, shape[1])
+    ws, wp, wb = _workspace(workspace, need[1], dev)
+    _check(lib().mxconv_linear_dgrad(s, pair(w.fmt, dz.fmt), w.codes.data_ptr(), w.scales.data_ptr(), dz.codes.data_ptr(),
+                                     dz.scales.data_ptr(), fn, _ptr(z), ldz, _ptr(add), lda, dx.data_ptr(), ldx, code, wp, wb,
+                                     _stream(stream)), "mxconv_linear_dgrad")
     return dx
 
 
@@ -721,19 +754,27 @@ def linear_wgrad(dz, x, bias=True, out=None, bias_out=None, workspace=None, stre
     """(dW, db): dZ^T X, fp32 [outs][ins], and the column sums of dZ, fp32
     [outs] (None with bias=False), from the MX matrices dZ [rows][outs] and
     X [rows][ins] (mxconv_linear_wgrad)."""
-    (rows, outs), (r2, ins), dev = _mx_matrix(dz, "dz"), _mx_matrix(x, "x"), x.codes.device
-    if r2 != rows or dz.codes.device != dev:
-        raise MxconvError(f"dz is {rows} x {outs} on {dz.codes.device}, x {r2} x {ins} on {dev}")
-    s, need = _linear_of(rows, outs, ins)
-    with _place(dev, stream):
-        dw = out if out is not None else torch.empty((outs, ins), dtype=torch.float32, device=dev)
+    (rows, outs, gdev), (r2, ins, dev) = _mx_matrix(dz, "dz"), _mx_matrix(x, "x")
+    if r2 != rows or gdev != dev:
+        raise MxconvError(f"dz is {rows} x {outs} on {gdev}, x {r2} x {ins} on {dev}")
+    return _linear_wgrad(rows, outs, ins, dz, x, bias, out, bias_out, workspace, dev, stream)
+
+
+@_placed
+def _linear_wgrad(rows, outs, ins, dz, x, bias, dw, db, workspace, dev, stream):
+    if dw is None:
+        dw = torch.empty((outs, ins), dtype=torch.float32, device=dev)
+    else:
         _vector(dw, "the output", (outs, ins), dev)
-        db = bias_out if bias_out is not None or not bias else torch.empty((outs,), dtype=torch.float32, device=dev)
+    if db is not None:
         _vector(db, "bias_out", (outs,), dev)
-        ws, wp, wb = _workspace(workspace, need[2], dev)
-        _check(lib().mxconv_linear_wgrad(ctypes.byref(s), pair(dz.fmt, x.fmt), _ptr(dz.codes), _ptr(dz.scales),
-                                         _ptr(x.codes), _ptr(x.scales), _ptr(dw), _ptr(db), wp, wb, _stream(stream)),
-               "mxconv_linear_wgrad")
+    elif bias:
+        db = torch.empty((outs,), dtype=torch.float32, device=dev)
+    s, need = _linear_of(rows, outs, ins)
+    ws, wp, wb = _workspace(workspace, need[2], dev)
+    _check(lib().mxconv_linear_wgrad(s, pair(dz.fmt, x.fmt), dz.codes.data_ptr(), dz.scales.data_ptr(), x.codes.data_ptr(),
+                                     x.scales.data_ptr(), dw.data_ptr(), _ptr(db), wp, wb, _stream(stream)),
+           "mxconv_linear_wgrad")
     return dw, db
 
 
@@ -746,8 +787,13 @@ def _norm_struct(y, w_post, gate, scale, w_pre, eps):
     if gate is not None and (gate.dim() != 2 or gate.shape[0] == 0 or rows % gate.shape[0]):
         raise MxconvError(f"gate must be [d] or [gates][d] with gates dividing the {rows} rows, got {tuple(gate.shape)}")
     gates = gate.shape[0] if gate is not None else 1
-    for t, what, shape in ((w_post, "w_post", (d,)), (w_pre, "w_pre", (d,)), (gate, "gate", (gates, d))):
-        _vector(t, what, shape, y.device)
+    dev = y.device
+    if w_post is not None:
+        _vector(w_post, "w_post", (d,), dev)
+    if w_pre is not None:
+        _vector(w_pre, "w_pre", (d,), dev)
+    if gate is not None:
+        _vector(gate, "gate", (gates, d), dev)
     return MxcNorm(rows, gates, d, _DTYPES[y.dtype], scale, eps, _ptr(w_post), _ptr(gate), _ptr(w_pre)), gates
 
 
@@ -763,17 +809,27 @@ def norm_residual(x, y, w_post=None, gate=None, scale=1.0, w_pre=None, eps=1e-6,
     = w . v / sqrt(mean(v^2) + eps) by rows (mxconv_norm_fwd).  x, y: [rows][d],
     fp32 or bf16; w_post, w_pre: fp32 [d] or None (N(y) is y; no U); gate: fp32
     [d], [gates][d] (each for rows / gates consecutive rows) or None."""
-    s, _ = _norm_struct(y, w_post, gate, scale, w_pre, eps)
-    (rows, d), dt, dev = y.shape, y.dtype, y.device
-    ldx, ldy = _rows_cols(x, "x", rows, d, dt, dev), _rows_cols(y, "y", rows, d, dt, dev)
-    with _place(dev, stream):
-        h = h_out if h_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
+    s, gates = _norm_struct(y, w_post, gate, scale, w_pre, eps)
+    return _norm_residual(s, x, y, w_pre is not None, h_out, u_out, y.device, stream)
+
+
+@_placed
+def _norm_residual(s, x, y, pre, h, u, dev, stream):
+    shape, dt = y.shape, y.dtype
+    ldx, ldy = _rows_cols(x, "x", shape, dt, dev), _rows_cols(y, "y", shape, dt, dev)
+    ldh = ldu = shape[1]
+    if h is None:
+        h = torch.empty(shape, dtype=dt, device=dev)
+    else:
+        ldh = _rows_cols(h, "h_out", shape, dt, dev)
+    if not pre:
         u = None
-        if w_pre is not None:
-            u = u_out if u_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
-        ldh, ldu = _rows_cols(h, "h_out", rows, d, dt, dev), _rows_cols(u, "u_out", rows, d, dt, dev)
-        _check(lib().mxconv_norm_fwd(ctypes.byref(s), _ptr(x), ldx, _ptr(y), ldy, _ptr(h), ldh, _ptr(u), ldu,
-                                     _stream(stream)), "mxconv_norm_fwd")
+    elif u is None:
+        u = torch.empty(shape, dtype=dt, device=dev)
+    else:
+        ldu = _rows_cols(u, "u_out", shape, dt, dev)
+    _check(lib().mxconv_norm_fwd(ctypes.byref(s), x.data_ptr(), ldx, y.data_ptr(), ldy, h.data_ptr(), ldh, _ptr(u), ldu,
+                                 _stream(stream)), "mxconv_norm_fwd")
     return h, u
 
 
@@ -784,23 +840,40 @@ def norm_residual_backward(dh, du, h, y, w_post=None, gate=None, scale=1.0, w_pr
     and h may be None without w_pre; the gradients of absent parameters are
     None; dgate is [gates][d]."""
     s, gates = _norm_struct(y, w_post, gate, scale, w_pre, eps)
-    (rows, d), dt, dev = y.shape, y.dtype, y.device
     if w_pre is None:
         du = h = None
     elif du is None or h is None:
         raise MxconvError("the backward pass of w_pre needs du and h")
-    lds = [_rows_cols(t, n, rows, d, dt, dev) for t, n in ((dh, "dh"), (du, "du"), (h, "h"), (y, "y"))]
-    with _place(dev, stream):
-        dx = dx_out if dx_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
-        dy = dy_out if dy_out is not None else torch.empty((rows, d), dtype=dt, device=dev)
-        lddx, lddy = _rows_cols(dx, "dx_out", rows, d, dt, dev), _rows_cols(dy, "dy_out", rows, d, dt, dev)
-        dw_pre, dw_post, dgate = (torch.empty(sh, dtype=torch.float32, device=dev) if t is not None else None
-                                  for t, sh in ((w_pre, (d,)), (w_post, (d,)), (gate, (gates, d))))
-        ws, wp, wb = _workspace(workspace, _norm_workspace_bytes(rows, gates, d, gate is not None, w_post is not None,
-                                                                 w_pre is not None), dev)
-        _check(lib().mxconv_norm_bwd(ctypes.byref(s), _ptr(dh), lds[0], _ptr(du), lds[1], _ptr(h), lds[2], _ptr(y), lds[3],
-                                     _ptr(dx), lddx, _ptr(dy), lddy, _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), wp, wb,
-                                     _stream(stream)), "mxconv_norm_bwd")
+    return _norm_backward(s, gates, dh, du, h, y, w_post is not None, gate is not None, dx_out, dy_out, workspace, y.device,
+                          stream)
+
+
+@_placed
+def _norm_backward(s, gates, dh, du, h, y, post, gate, dx, dy, workspace, dev, stream):
+    shape, dt = y.shape, y.dtype
+    rows, d = shape
+    lddh, ldy = _rows_cols(dh, "dh", shape, dt, dev), _rows_cols(y, "y", shape, dt, dev)
+    lddu = ldh = lddx = lddy = d
+    dw_pre = dw_post = dgate = None
+    if h is not None:
+        lddu, ldh = _rows_cols(du, "du", shape, dt, dev), _rows_cols(h, "h", shape, dt, dev)
+        dw_pre = torch.empty((d,), dtype=torch.float32, device=dev)
+    if dx is None:
+        dx = torch.empty(shape, dtype=dt, device=dev)
+    else:
+        lddx = _rows_cols(dx, "dx_out", shape, dt, dev)
+    if dy is None:
+        dy = torch.empty(shape, dtype=dt, device=dev)
+    else:
+        lddy = _rows_cols(dy, "dy_out", shape, dt, dev)
+    if post:
+        dw_post = torch.empty((d,), dtype=torch.float32, device=dev)
+    if gate:
+        dgate = torch.empty((gates, d), dtype=torch.float32, device=dev)
+    ws, wp, wb = _workspace(workspace, _norm_workspace_bytes(rows, gates, d, gate, post, h is not None), dev)
+    _check(lib().mxconv_norm_bwd(ctypes.byref(s), dh.data_ptr(), lddh, _ptr(du), lddu, _ptr(h), ldh, y.data_ptr(), ldy,
+                                 dx.data_ptr(), lddx, dy.data_ptr(), lddy, _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), wp, wb,
+                                 _stream(stream)), "mxconv_norm_bwd")
     return dx, dy, dw_pre, dw_post, dgate
 
 
@@ -840,13 +913,18 @@ def _clip(tensors, outs, max_norm, norm_out, workspace, stream):
         desc[1::4] = array("q", dst)
         if len(set(dst)) != len(dst) and len(set(full := [p for p, n in zip(dst, sizes) if n])) != len(full):
             raise MxconvError("a tensor is written twice")
-    with _place(dev, stream):
-        norm = norm_out if norm_out is not None else torch.empty((), dtype=torch.float32, device=dev)
-        if norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != dev:
-            raise MxconvError(f"norm_out must be one fp32 element on {dev}")
-        ws, wp, wb = _workspace(workspace, _clip_workspace_bytes(), dev)
-        _check(lib().mxconv_grad_clip(len(ptrs), desc.buffer_info()[0], max_norm, _ptr(norm), wp, wb, _stream(stream)),
-               "mxconv_grad_clip")
+    return _clip_launch(len(ptrs), desc, max_norm, norm_out, workspace, dev, stream)
+
+
+@_placed
+def _clip_launch(count, desc, max_norm, norm, workspace, dev, stream):
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=dev)
+    elif norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != dev:
+        raise MxconvError(f"norm_out must be one fp32 element on {dev}")
+    ws, wp, wb = _workspace(workspace, _clip_workspace_bytes(), dev)
+    _check(lib().mxconv_grad_clip(count, desc.buffer_info()[0], max_norm, norm.data_ptr(), wp, wb, _stream(stream)),
+           "mxconv_grad_clip")
     return norm
 
 

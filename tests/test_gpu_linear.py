@@ -46,11 +46,13 @@ def _fwd_ref(x, w, bias, fn, res):
     return z, tz, y, ty
 
 
-# rows, ins, outs: one row; a few rows with a split contraction; 33..64 rows;
+# rows, ins, outs: one row; a few rows; 33..64 rows;
 # one 32-block; odd everything; several tiles; a wide tile grid with a ragged edge
 SIZES = [(1, 64, 96), (1, 1000, 37), (5, 4500, 70), (31, 32, 33), (47, 260, 300), (64, 2080, 129), (65, 96, 65),
          (130, 1, 1), (200, 777, 515), (700, 333, 1030), (1300, 130, 1250),
-         (2100, 200, 1990), (1900, 2030, 260)]
+         (2100, 200, 1990), (1900, 2030, 260),
+         # long contractions of each product, split over workgroups
+         (3, 9000, 70), (9000, 40, 70), (40, 70, 9000), (100, 8300, 90)]
 
 
 @pytest.mark.parametrize("fmt", list(mm.FORMATS))
@@ -213,9 +215,9 @@ def test_rows_do_not_see_each_other(mx):
 
 def test_repeated_calls_are_bit_equal(mx):
     """Split contractions are joined in a fixed order."""
-    x, _ = mm.matrix(mx, 3000, 200, 0, 1)
-    dz, _ = mm.matrix(mx, 3000, 96, 0, 2)
-    assert mx.linear_workspace_bytes(mx.LINEAR_WGRAD, 3000, 96, 200) > 0
+    x, _ = mm.matrix(mx, 9000, 200, 0, 1)
+    dz, _ = mm.matrix(mx, 9000, 96, 0, 2)
+    assert mx.linear_workspace_bytes(mx.LINEAR_WGRAD, 9000, 96, 200) > 0
     first = mx.linear_wgrad(dz, x)
     for _ in range(4):
         again = mx.linear_wgrad(dz, x)
