@@ -797,6 +797,12 @@ def _norm_struct(y, w_post, gate, scale, w_pre, eps):
     return MxcNorm(rows, gates, d, _DTYPES[y.dtype], scale, eps, _ptr(w_post), _ptr(gate), _ptr(w_pre)), gates
 
 
+def norm_workspace_bytes(rows, d, gates=1, gate=True, post=True, pre=True):
+    """Workspace of norm_residual_backward for `rows` rows of length d with
+    these parameters (with fewer parameters it is no larger)."""
+    return _norm_workspace_bytes(rows, gates, d, gate, post, pre)
+
+
 @functools.lru_cache(maxsize=_CACHED)
 def _norm_workspace_bytes(rows, gates, d, gate, post, pre):
     some = 16                                         # only whether a pointer is NULL is looked at
@@ -834,7 +840,7 @@ def _norm_residual(s, x, y, pre, h, u, dev, stream):
 
 
 def norm_residual_backward(dh, du, h, y, w_post=None, gate=None, scale=1.0, w_pre=None, eps=1e-6, dx_out=None, dy_out=None,
-                           workspace=None, stream=None):
+                           dw_pre_out=None, dw_post_out=None, dgate_out=None, workspace=None, stream=None):
     """(dX, dY, dw_pre, dw_post, dgate) of norm_residual from the gradients dh
     of H and du of U, with H and y of the forward pass (mxconv_norm_bwd).  du
     and h may be None without w_pre; the gradients of absent parameters are
@@ -844,20 +850,29 @@ def norm_residual_backward(dh, du, h, y, w_post=None, gate=None, scale=1.0, w_pr
         du = h = None
     elif du is None or h is None:
         raise MxconvError("the backward pass of w_pre needs du and h")
-    return _norm_backward(s, gates, dh, du, h, y, w_post is not None, gate is not None, dx_out, dy_out, workspace, y.device,
-                          stream)
+    return _norm_backward(s, gates, dh, du, h, y, w_post is not None, gate is not None, dx_out, dy_out, dw_pre_out, dw_post_out,
+                          dgate_out, workspace, y.device, stream)
+
+
+def _result(t, what, shape, dev):
+    """An fp32 output: the caller's, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=torch.float32, device=dev)
+    _vector(t, what, shape, dev)
+    return t
 
 
 @_placed
-def _norm_backward(s, gates, dh, du, h, y, post, gate, dx, dy, workspace, dev, stream):
+def _norm_backward(s, gates, dh, du, h, y, post, gate, dx, dy, dw_pre, dw_post, dgate, workspace, dev, stream):
     shape, dt = y.shape, y.dtype
     rows, d = shape
     lddh, ldy = _rows_cols(dh, "dh", shape, dt, dev), _rows_cols(y, "y", shape, dt, dev)
     lddu = ldh = lddx = lddy = d
-    dw_pre = dw_post = dgate = None
     if h is not None:
         lddu, ldh = _rows_cols(du, "du", shape, dt, dev), _rows_cols(h, "h", shape, dt, dev)
-        dw_pre = torch.empty((d,), dtype=torch.float32, device=dev)
+    dw_pre = _result(dw_pre, "dw_pre_out", (d,), dev) if h is not None else None
+    dw_post = _result(dw_post, "dw_post_out", (d,), dev) if post else None
+    dgate = _result(dgate, "dgate_out", (gates, d), dev) if gate else None
     if dx is None:
         dx = torch.empty(shape, dtype=dt, device=dev)
     else:
@@ -866,10 +881,6 @@ def _norm_backward(s, gates, dh, du, h, y, post, gate, dx, dy, workspace, dev, s
         dy = torch.empty(shape, dtype=dt, device=dev)
     else:
         lddy = _rows_cols(dy, "dy_out", shape, dt, dev)
-    if post:
-        dw_post = torch.empty((d,), dtype=torch.float32, device=dev)
-    if gate:
-        dgate = torch.empty((gates, d), dtype=torch.float32, device=dev)
     ws, wp, wb = _workspace(workspace, _norm_workspace_bytes(rows, gates, d, gate, post, h is not None), dev)
     _check(lib().mxconv_norm_bwd(ctypes.byref(s), dh.data_ptr(), lddh, _ptr(du), lddu, _ptr(h), ldh, y.data_ptr(), ldy,
                                  dx.data_ptr(), lddx, dy.data_ptr(), lddy, _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), wp, wb,

@@ -153,6 +153,22 @@ def real_flops(node, n):
     return 2.0 * n * node["cout"] * node["h"] * node["w"] * node["cin_real"] * node["k"] * node["k"]
 
 
+class _Clip:
+    """The gradient clipping at the end of a step (or its absence)."""
+
+    def __init__(self, max_norm, device):
+        self.max_norm = max_norm
+        if max_norm is not None:
+            self.norm = torch.zeros((), dtype=torch.float32, device=device)
+            self.ws = torch.empty(mx.lib().mxconv_grad_clip_workspace_bytes(), dtype=torch.uint8, device=device)
+
+    def calls(self, grads):
+        if self.max_norm is None:
+            return []
+        return [("clip", lambda: mx.grad_clip(grads, self.max_norm, norm_out=self.norm, workspace=self.ws), 0.0,
+                 8.0 * sum(g.numel() for g in grads))]
+
+
 # ---------------------------------------------------------------- the step
 class NetStep:
     """Buffers and the call sequence of one fwd+bwd training step of `net`
@@ -166,9 +182,13 @@ class NetStep:
     Full-precision tensors between layers (pre-activations, input gradients,
     upstream gradients) are kept in `master`: bf16 by default, each GEMM
     result rounded to bf16 before it is activated, multiplied or quantized
-    (the library's MXC_FN_BF16 / MXC_CBF_BF16 mode), or fp32."""
+    (the library's MXC_FN_BF16 / MXC_CBF_BF16 mode), or fp32.
 
-    def __init__(self, net, n, fmt, device, seed=3000, fused_dgrad=True, master=torch.bfloat16):
+    clip: the step ends by scaling all weight gradients, in place, to at most
+    this Euclidean norm together (mxconv_grad_clip); their norm before that
+    is left in clip.norm.  None: they are left as they are."""
+
+    def __init__(self, net, n, fmt, device, seed=3000, fused_dgrad=True, master=torch.bfloat16, clip=None):
         if n % 32:
             raise ValueError("the network step runs batch blocks of 32")
         if master not in (torch.bfloat16, torch.float32):
@@ -180,6 +200,7 @@ class NetStep:
         self.es = 2.0 if bf else 4.0                       # bytes per full-precision element
         self.fbf = mx.FN_BF16 if bf else 0                 # fn flag of the fused calls
         self.gx_layout = mx.CBF_BF16 if bf else mx.CBF
+        self.clip = _Clip(clip, device)
         self.convs = net.convs()
         img = net.nodes[0]
         self.image = synth.uniform((n, img["c"], img["h"], img["w"]), seed).to(torch.bfloat16).to(device)
@@ -353,7 +374,7 @@ class NetStep:
             by = sum((mx.wgrad_workspace_bytes(cv, fmt) + 4.0 * gw.numel()) if mx.wgrad_workspace_bytes(cv, fmt) else 0.0
                      for cv, _, _, gw in grp)
             seq.append((f"wgrad_reduce{i // mx.WREDUCE_MAX}", lambda grp=grp: mx.wgrad_reduce_multi(grp), 0.0, by))
-        return seq
+        return seq + self.clip.calls([self.gw[nm] for nm in names])
 
     def flops(self):
         """Algorithmic flops of the step's GEMMs (real channels): forward,
@@ -377,16 +398,18 @@ class QlrStep:
     256 -> 256 three times, SiLU) runs fwd + bwd on batches of 128 = three
     replayed 32-sample groups (copied as stored codes, never requantized)
     and 32 fresh inputs (front stack forward, quantized once by its last
-    epilogue straight into the batch).  Upstream gradient ~ N(0, 1e-3)."""
+    epilogue straight into the batch).  Upstream gradient ~ N(0, 1e-3).
+    clip: as in NetStep."""
 
     FRONT = ((3, 32), (32, 64), (64, 128))
     BACK = ((128, 256), (256, 256), (256, 256), (256, 256))
 
     def __init__(self, device, fmt=mx.E2M1, buffer=8192, batch=128, seed=5000, fused_dgrad=True,
-                 master=torch.bfloat16):
+                 master=torch.bfloat16, clip=None):
         if master not in (torch.bfloat16, torch.float32):
             raise ValueError("master tensors are bf16 or fp32")
         self.dev, self.fmt, self.batch = device, fmt, batch
+        self.clip = _Clip(clip, device)
         self.fused = fused_dgrad
         bf = master == torch.bfloat16
         self.es = 2.0 if bf else 4.0
@@ -524,7 +547,7 @@ class QlrStep:
                  if mx.wgrad_workspace_bytes(cv, fmt))
         seq.append(("wgrad_reduce", lambda: mx.wgrad_reduce_multi(
             [(cv, fmt, self.ws[i], self.gw[i]) for i, cv in enumerate(self.back_cv)]), 0.0, rb))
-        return seq
+        return seq + self.clip.calls(self.gw)
 
     def flops(self):
         """Back stack: forward, input gradient (not for the first layer) and
@@ -538,3 +561,88 @@ class QlrStep:
             ho, wo = synth.out_hw(cv)
             tot += 2.0 * cv["n"] * cv["cout"] * ho * wo * cv["cin"] * 9
         return tot
+
+
+# ---------------------------------------------------------------- a residual block of linear layers
+class BlockStep:
+    """One fwd+bwd training step of a residual block of two linear layers on
+    `rows` samples (tokens, or pixels of a feature map) of width `dim`, hidden
+    width `hidden`, in MX format fmt, every matrix quantized once:
+
+        H = X + scale gate . N(Y; w_post),  U = N(H; w_pre)    (the block before's output Y joins the stream)
+        Z = U W1^T + b1,  O = silu(Z) W2^T + b2 + H
+
+    Inputs (seeded): X, Y ~ N(0, 1) and the upstream gradient of O ~ N(0,
+    1e-3) in `master` (bf16 or fp32); fp32 parameters.  The gradients of X, Y
+    (dx, dy) and of every parameter (grads, in the order of `params`), the
+    latter scaled together to at most the norm `clip` (None: left as they
+    are)."""
+
+    def __init__(self, rows, dim, hidden, fmt, device, seed=7000, master=torch.bfloat16, clip=1.0):
+        if master not in (torch.bfloat16, torch.float32):
+            raise ValueError("master tensors are bf16 or fp32")
+        self.rows, self.dim, self.hidden, self.fmt, self.dt = rows, dim, hidden, fmt, master
+        self.scale, self.eps = 0.7, 1e-6
+        self.es = 2.0 if master == torch.bfloat16 else 4.0
+
+        def normal(shape, std, k, dtype=torch.float32, mean=0.0):
+            return (synth.normal(shape, std, seed + k) + mean).to(dtype).to(device)
+
+        def matrix(r, c):
+            return mx.MxTensor.empty(mx.WEIGHT, fmt, (r, c, 1, 1), device)
+
+        self.x, self.y = normal((rows, dim), 1.0, 0, master), normal((rows, dim), 1.0, 1, master)
+        self.do = normal((rows, dim), 1e-3, 2, master)
+        self.params = {"w1": normal((hidden, dim), dim ** -0.5, 3), "b1": normal((hidden,), 0.1, 4),
+                       "w2": normal((dim, hidden), hidden ** -0.5, 5), "b2": normal((dim,), 0.1, 6),
+                       "w_pre": normal((dim,), 0.1, 7, mean=1.0), "w_post": normal((dim,), 0.1, 8, mean=1.0),
+                       "gate": normal((1, dim), 0.5, 9)}
+        self.grads = {k: torch.empty_like(v) for k, v in self.params.items()}
+        self.w1, self.w2 = matrix(hidden, dim), matrix(dim, hidden)
+        self.u_q, self.a_q, self.do_q, self.dz_q = (matrix(rows, c) for c in (dim, hidden, dim, hidden))
+        self.h, self.u, self.o, self.du, self.dx, self.dy = (torch.empty_like(self.x) for _ in range(6))
+        self.z, self.a, self.dz = (torch.empty((rows, hidden), dtype=master, device=device) for _ in range(3))
+        self.clip = _Clip(clip, device)
+
+        def ws(n):
+            return torch.empty(max(16, n), dtype=torch.uint8, device=device)
+
+        self.ws = [ws(max(mx.linear_workspace_bytes(op, rows, o, i) for op in range(3)))
+                   for o, i in ((hidden, dim), (dim, hidden))]
+        self.nws = ws(mx.norm_workspace_bytes(rows, dim))
+
+    def calls(self):
+        """The step as (label, callable, algorithmic flops, algorithmic bytes)
+        tuples, with the conventions of NetStep.calls."""
+        p, g, q, dt, fmt = self.params, self.grads, mx.quantize_matrix, self.dt, self.fmt
+        m, d, f = self.rows, self.dim, self.hidden
+        norm = dict(w_post=p["w_post"], gate=p["gate"], scale=self.scale, w_pre=p["w_pre"], eps=self.eps)
+        mm = 2.0 * m * d * f
+        es, W = self.es, mx.WEIGHT
+
+        def b(r, c):
+            return mxb(W, fmt, (r, c, 1, 1))
+
+        seq = [("quant_w", lambda: (q(p["w1"], fmt, out=self.w1), q(p["w2"], fmt, out=self.w2)), 0.0,
+                8.0 * d * f + 2 * b(f, d)),
+               ("norm", lambda: mx.norm_residual(self.x, self.y, h_out=self.h, u_out=self.u, **norm), 0.0, 4 * es * m * d),
+               ("quant_u", lambda: q(self.u, fmt, out=self.u_q), 0.0, es * m * d + b(m, d)),
+               ("linear1", lambda: mx.linear(self.w1, self.u_q, bias=p["b1"], fn=mx.FN_SILU, dtype=dt, out=self.a,
+                                             pre_out=self.z, workspace=self.ws[0]), mm, b(f, d) + b(m, d) + 2 * es * m * f),
+               ("quant_a", lambda: q(self.a, fmt, out=self.a_q), 0.0, es * m * f + b(m, f)),
+               ("linear2", lambda: mx.linear(self.w2, self.a_q, bias=p["b2"], residual=self.h, dtype=dt, out=self.o,
+                                             workspace=self.ws[1]), mm, b(f, d) + b(m, f) + 2 * es * m * d),
+               ("quant_do", lambda: q(self.do, fmt, out=self.do_q), 0.0, es * m * d + b(m, d)),
+               ("dgrad2", lambda: mx.linear_dgrad(self.w2, self.do_q, fn=mx.FN_SILU, z=self.z, dtype=dt, out=self.dz,
+                                                  workspace=self.ws[1]), mm, b(f, d) + b(m, d) + 2 * es * m * f),
+               ("wgrad2", lambda: mx.linear_wgrad(self.do_q, self.a_q, out=g["w2"], bias_out=g["b2"], workspace=self.ws[1]),
+                mm, b(m, d) + b(m, f) + 4.0 * d * f),
+               ("quant_dz", lambda: q(self.dz, fmt, out=self.dz_q), 0.0, es * m * f + b(m, f)),
+               ("dgrad1", lambda: mx.linear_dgrad(self.w1, self.dz_q, dtype=dt, out=self.du, workspace=self.ws[0]), mm,
+                b(f, d) + b(m, f) + es * m * d),
+               ("wgrad1", lambda: mx.linear_wgrad(self.dz_q, self.u_q, out=g["w1"], bias_out=g["b1"], workspace=self.ws[0]),
+                mm, b(m, d) + b(m, f) + 4.0 * d * f),
+               ("norm_bwd", lambda: mx.norm_residual_backward(
+                   self.do, self.du, self.h, self.y, dx_out=self.dx, dy_out=self.dy, dw_pre_out=g["w_pre"],
+                   dw_post_out=g["w_post"], dgate_out=g["gate"], workspace=self.nws, **norm), 0.0, 6 * es * m * d)]
+        return seq + self.clip.calls(list(g.values()))
