@@ -6,7 +6,6 @@
 namespace mxc {
 
 constexpr int NORM_MAX_DIM = 8192;
-constexpr int NORM_FWD_RUNS = 4096;
 
 // Threads that share a row, and the values of it that each holds: 8, so that
 // four waves a SIMD fit, but 16 for the longest rows (a row of 8192 on 1024
@@ -21,7 +20,10 @@ inline int norm_tpr(int d) {
 // least 256), backward ones 512, for fewer partial sums
 inline int norm_fwd_rows(int d) { return norm_tpr(d) == 64 ? 4 : 1; }
 inline int norm_bwd_rows(int d) { return 512 / norm_tpr(d); }
-// backward workgroups, so partial column sums: what the CUs hold at once
+// Workgroups, each with a run of rows: what the CUs hold at once (16 waves a CU,
+// by registers), so that no part of the grid is left for a second round;
+// backward it is also the number of partial column sums.
+inline int norm_fwd_runs(int d) { return norm_tpr(d) == 64 ? 1024 : 256 * 16 / (norm_tpr(d) / 64); }
 inline int norm_runs(int d) { return norm_vals(d) == 8 ? 512 : 256; }
 
 struct NormArgs {

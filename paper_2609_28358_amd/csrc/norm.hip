@@ -36,35 +36,43 @@ struct __attribute__((packed, aligned(4))) Raw16f {
 template <typename T> using Raw = std::conditional_t<sizeof(T) == 2, Raw16, Raw16f>;
 
 template <typename T>
-__device__ __forceinline__ float ld1(const T* p) {
-    if constexpr (sizeof(T) == 4) return *p;
-    else return __uint_as_float((uint32_t)*(const uint16_t*)p << 16);
-}
-template <typename T>
 __device__ __forceinline__ void st1(T* p, float v) {
     if constexpr (sizeof(T) == 4) *p = v;
     else *(uint16_t*)p = (uint16_t)bf16_bits(v);
 }
-// n: values of the row left from here on
+// n: values of the row left from here on.  get() reads a vector as it is stored,
+// unpack() makes floats of it; the rows' loops read one row ahead.
 template <typename T>
-__device__ __forceinline__ void ld(const T* p, int n, float* o) {
+__device__ __forceinline__ Raw<T> get(const T* p, int n) {
     constexpr int V = VEC<T>;
-    if (n >= V) {
-        const Raw<T> u = *(const Raw<T>*)p;
+    if (n >= V) return *(const Raw<T>*)p;
+    Raw<T> u;
 #pragma unroll
-        for (int k = 0; k < 4; k++) {
-            if constexpr (V == 8) {
-                o[2 * k] = __uint_as_float(u.w[k] << 16);
-                o[2 * k + 1] = __uint_as_float(u.w[k] & 0xFFFF0000u);
-            } else {
-                o[k] = __uint_as_float(u.w[k]);
-            }
+    for (int k = 0; k < 4; k++) {
+        if constexpr (V == 8) {
+            const uint32_t lo = 2 * k < n ? *(const uint16_t*)(p + 2 * k) : 0u;
+            const uint32_t hi = 2 * k + 1 < n ? *(const uint16_t*)(p + 2 * k + 1) : 0u;
+            u.w[k] = lo | hi << 16;
+        } else {
+            u.w[k] = k < n ? __float_as_uint(p[k]) : 0u;
         }
-    } else {
+    }
+    return u;
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw<T>& u, float* o) {
 #pragma unroll
-        for (int e = 0; e < V; e++) o[e] = e < n ? ld1(p + e) : 0.0f;
+    for (int k = 0; k < 4; k++) {
+        if constexpr (VEC<T> == 8) {
+            o[2 * k] = __uint_as_float(u.w[k] << 16);
+            o[2 * k + 1] = __uint_as_float(u.w[k] & 0xFFFF0000u);
+        } else {
+            o[k] = __uint_as_float(u.w[k]);
+        }
     }
 }
+template <typename T>
+__device__ __forceinline__ void ld(const T* p, int n, float* o) { unpack<T>(get(p, n), o); }
 template <typename T>
 __device__ __forceinline__ void st(T* p, int n, const float* v) {
     constexpr int V = VEC<T>;
@@ -136,7 +144,7 @@ __device__ __forceinline__ void columns(int d, int t, F&& f) {
 }
 
 template <typename T, int NV, int TPR>
-__global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NV == 8 ? 4 : 2) void norm_fwd_kernel(const NormArgs a) {
+__global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NV == 8 || sizeof(T) == 2 ? 4 : 2) void norm_fwd_kernel(const NormArgs a) {
     constexpr int V = VEC<T>;
     constexpr int RL = TPR == 64 ? 4 : 1;             // rows a workgroup takes at a time
     __shared__ float red[2][TPR / 64];
@@ -149,6 +157,14 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NV == 8 ? 4 : 2) void norm_f
         if (a.w_pre) ldp<V>(a.w_pre + c, n, wq + q);
     });
     long long gate = -1;
+    Raw<T> nx[NV / V], ny[NV / V];
+    auto fetch = [&](long long r) {
+        columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
+            nx[q / V] = get((const T*)a.x + r * a.ldx + c, n);
+            ny[q / V] = get((const T*)a.y + r * a.ldy + c, n);
+        });
+    };
+    if (first + rl < last) fetch(first + rl);
     for (long long r = first + rl; r < last; r += RL) {
         const long long gr = a.gate ? r / a.gate_rows : 0;
         if (gr != gate) {                                     // s g, for this gate's rows
@@ -162,11 +178,12 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NV == 8 ? 4 : 2) void norm_f
         }
         float x[NV], y[NV], s[1] = {0.0f};
         columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
-            ld<T>((const T*)a.x + r * a.ldx + c, n, x + q);
-            ld<T>((const T*)a.y + r * a.ldy + c, n, y + q);
+            unpack<T>(nx[q / V], x + q);
+            unpack<T>(ny[q / V], y + q);
 #pragma unroll
             for (int e = 0; e < V; e++) s[0] += y[q + e] * y[q + e];
         });
+        if (r + RL < last) fetch(r + RL);
         float ry = 1.0f;
         if (a.w_post) {
             row_sum<TPR, 1>(s, red, par);
@@ -253,18 +270,46 @@ __global__ __launch_bounds__(512, NV == 8 ? 4 : 2) void norm_bwd_kernel(const No
         });
         // the workgroup's rows in step, for the barriers of their sums: where the
         // last ones do not exist, the run's last row is computed and dropped
+        // bf16 rows are read one ahead; fp32 ones leave no registers for that
+        constexpr bool AHEAD = sizeof(T) == 2;
+        constexpr int NR = AHEAD ? NV / V : 1;
+        Raw<T> nx[NR], ny[NR], nh[NR], nu[NR];
+        auto fetch = [&](long long rb) {
+            const long long r = gr * a.gate_rows + min(rb + rl, o1 - 1);
+            columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
+                nx[q / V % NR] = get((const T*)a.x + r * a.ldx + c, n);  // dH
+                ny[q / V % NR] = get((const T*)a.y + r * a.ldy + c, n);
+                if (a.w_pre) {
+                    nh[q / V % NR] = get((const T*)a.h + r * a.ldh + c, n);
+                    nu[q / V % NR] = get((const T*)a.u + r * a.ldu + c, n);   // dU
+                }
+            });
+        };
+        if constexpr (AHEAD) fetch(o0);
         for (long long rb = o0; rb < o1; rb += RL) {
             const bool live = rb + rl < o1;
             const long long r = gr * a.gate_rows + (live ? rb + rl : o1 - 1);
             float x[NV], y[NV], h[NV], du[NV], s[3] = {0.0f, 0.0f, 0.0f};
             columns<V, NV, TPR>(d, t, [&](int q, int c, int n) {
-                ld<T>((const T*)a.x + r * a.ldx + c, n, x + q);          // dH
-                ld<T>((const T*)a.y + r * a.ldy + c, n, y + q);
-                if (a.w_pre) {
-                    ld<T>((const T*)a.h + r * a.ldh + c, n, h + q);
-                    ld<T>((const T*)a.u + r * a.ldu + c, n, du + q);     // dU
+                if constexpr (AHEAD) {
+                    unpack<T>(nx[q / V], x + q);
+                    unpack<T>(ny[q / V], y + q);
+                    if (a.w_pre) {
+                        unpack<T>(nh[q / V], h + q);
+                        unpack<T>(nu[q / V], du + q);
+                    }
+                } else {
+                    ld<T>((const T*)a.x + r * a.ldx + c, n, x + q);
+                    ld<T>((const T*)a.y + r * a.ldy + c, n, y + q);
+                    if (a.w_pre) {
+                        ld<T>((const T*)a.h + r * a.ldh + c, n, h + q);
+                        ld<T>((const T*)a.u + r * a.ldu + c, n, du + q);
+                    }
                 }
             });
+            if constexpr (AHEAD) {
+                if (rb + RL < o1) fetch(rb + RL);
+            }
             columns<V, NV, TPR>(d, t, [&](int q, int, int) {
 #pragma unroll
                 for (int e = 0; e < V; e++) {
@@ -428,7 +473,7 @@ void plan_runs(NormArgs& a) {
 
 int launch_norm_fwd(NormArgs a, bool bf16, hipStream_t s) {
     const long long rl = norm_fwd_rows(a.d);
-    a.run = std::max<long long>(rl, (a.rows + NORM_FWD_RUNS - 1) / NORM_FWD_RUNS);
+    a.run = std::max<long long>(rl, (a.rows + norm_fwd_runs(a.d) - 1) / norm_fwd_runs(a.d));
     return launch(a, false, bf16, (unsigned)((a.rows + a.run - 1) / a.run), s);
 }
 

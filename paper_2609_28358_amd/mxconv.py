@@ -714,7 +714,7 @@ def linear(w, x, bias=None, fn=FN_NONE, residual=None, dtype=torch.bfloat16, out
 @_placed
 def _linear(shape, ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace, dev, stream):
     code = _dtype_code(dtype)
-    y = out if out is not None else torch.empty(shape, dtype=dtype, device=dev)
+    y = out if out is not None else x.codes.new_empty(shape, dtype=dtype)
     ldr = _rows_cols(residual, "residual", shape, dtype, dev) if residual is not None else 0
     ldz = _rows_cols(pre_out, "pre_out", shape, dtype, dev) if pre_out is not None else 0
     ldy = _rows_cols(y, "the output", shape, dtype, dev) if out is not None else shape[1]
@@ -738,7 +738,7 @@ def linear_dgrad(w, dz, fn=FN_NONE, z=None, add=None, dtype=torch.bfloat16, out=
 @_placed
 def _linear_dgrad(shape, outs, w, dz, fn, z, add, dtype, out, workspace, dev, stream):
     code = _dtype_code(dtype)
-    dx = out if out is not None else torch.empty(shape, dtype=dtype, device=dev)
+    dx = out if out is not None else dz.codes.new_empty(shape, dtype=dtype)
     ldz = _rows_cols(z, "z", shape, dtype, dev) if z is not None else 0
     lda = _rows_cols(add, "add", shape, dtype, dev) if add is not None else 0
     ldx = _rows_cols(dx, "the output", shape, dtype, dev) if out is not None else shape[1]
@@ -763,13 +763,13 @@ def linear_wgrad(dz, x, bias=True, out=None, bias_out=None, workspace=None, stre
 @_placed
 def _linear_wgrad(rows, outs, ins, dz, x, bias, dw, db, workspace, dev, stream):
     if dw is None:
-        dw = torch.empty((outs, ins), dtype=torch.float32, device=dev)
+        dw = x.codes.new_empty((outs, ins), dtype=torch.float32)
     else:
         _vector(dw, "the output", (outs, ins), dev)
     if db is not None:
         _vector(db, "bias_out", (outs,), dev)
     elif bias:
-        db = torch.empty((outs,), dtype=torch.float32, device=dev)
+        db = x.codes.new_empty((outs,), dtype=torch.float32)
     s, need = _linear_of(rows, outs, ins)
     ws, wp, wb = _workspace(workspace, need[2], dev)
     _check(lib().mxconv_linear_wgrad(s, pair(dz.fmt, x.fmt), dz.codes.data_ptr(), dz.scales.data_ptr(), x.codes.data_ptr(),
@@ -822,16 +822,17 @@ def norm_residual(x, y, w_post=None, gate=None, scale=1.0, w_pre=None, eps=1e-6,
 @_placed
 def _norm_residual(s, x, y, pre, h, u, dev, stream):
     shape, dt = y.shape, y.dtype
+    # a row-major y (checked here): empty_like() is contiguous
     ldx, ldy = _rows_cols(x, "x", shape, dt, dev), _rows_cols(y, "y", shape, dt, dev)
     ldh = ldu = shape[1]
     if h is None:
-        h = torch.empty(shape, dtype=dt, device=dev)
+        h = torch.empty_like(y)
     else:
         ldh = _rows_cols(h, "h_out", shape, dt, dev)
     if not pre:
         u = None
     elif u is None:
-        u = torch.empty(shape, dtype=dt, device=dev)
+        u = torch.empty_like(y)
     else:
         ldu = _rows_cols(u, "u_out", shape, dt, dev)
     _check(lib().mxconv_norm_fwd(ctypes.byref(s), x.data_ptr(), ldx, y.data_ptr(), ldy, h.data_ptr(), ldh, _ptr(u), ldu,
@@ -854,10 +855,10 @@ def norm_residual_backward(dh, du, h, y, w_post=None, gate=None, scale=1.0, w_pr
                           dgate_out, workspace, y.device, stream)
 
 
-def _result(t, what, shape, dev):
-    """An fp32 output: the caller's, or a new one."""
+def _result(t, what, shape, dev, like):
+    """An fp32 output: the caller's, or a new one (like another tensor)."""
     if t is None:
-        return torch.empty(shape, dtype=torch.float32, device=dev)
+        return like.new_empty(shape, dtype=torch.float32)
     _vector(t, what, shape, dev)
     return t
 
@@ -870,15 +871,15 @@ def _norm_backward(s, gates, dh, du, h, y, post, gate, dx, dy, dw_pre, dw_post, 
     lddu = ldh = lddx = lddy = d
     if h is not None:
         lddu, ldh = _rows_cols(du, "du", shape, dt, dev), _rows_cols(h, "h", shape, dt, dev)
-    dw_pre = _result(dw_pre, "dw_pre_out", (d,), dev) if h is not None else None
-    dw_post = _result(dw_post, "dw_post_out", (d,), dev) if post else None
-    dgate = _result(dgate, "dgate_out", (gates, d), dev) if gate else None
+    dw_pre = _result(dw_pre, "dw_pre_out", (d,), dev, y) if h is not None else None
+    dw_post = _result(dw_post, "dw_post_out", (d,), dev, y) if post else None
+    dgate = _result(dgate, "dgate_out", (gates, d), dev, y) if gate else None
     if dx is None:
-        dx = torch.empty(shape, dtype=dt, device=dev)
+        dx = torch.empty_like(y)
     else:
         lddx = _rows_cols(dx, "dx_out", shape, dt, dev)
     if dy is None:
-        dy = torch.empty(shape, dtype=dt, device=dev)
+        dy = torch.empty_like(y)
     else:
         lddy = _rows_cols(dy, "dy_out", shape, dt, dev)
     ws, wp, wb = _workspace(workspace, _norm_workspace_bytes(rows, gates, d, gate, post, h is not None), dev)
