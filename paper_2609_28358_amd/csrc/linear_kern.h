@@ -143,32 +143,40 @@ __device__ __forceinline__ float lin_value(int fn, float v, float b, float z, fl
 template <int BYTES, int AL> struct __attribute__((packed, aligned(AL))) LinRaw {
     uint32_t w[BYTES / 4];
 };
+template <bool BF, int N> using LinVec = LinRaw<BF ? 2 * N : 4 * N, BF ? 2 : 4>;
 template <bool BF, int N>
-__device__ __forceinline__ void lin_load(const void* base, long long i, int left, float* o) {
+__device__ __forceinline__ LinVec<BF, N> lin_get(const void* base, long long i, int left) {
+    LinVec<BF, N> u;
     if constexpr (BF) {
         const uint16_t* p = (const uint16_t*)base + i;
-        if (left >= N) {
-            const LinRaw<2 * N, 2> u = *(const LinRaw<2 * N, 2>*)p;
+        if (left >= N) return *(const LinVec<BF, N>*)p;
 #pragma unroll
-            for (int k = 0; k < N / 2; k++) {
-                o[2 * k] = __uint_as_float(u.w[k] << 16);
-                o[2 * k + 1] = __uint_as_float(u.w[k] & 0xFFFF0000u);
-            }
-        } else {
+        for (int k = 0; k < N / 2; k++)
+            u.w[k] = (2 * k < left ? p[2 * k] : 0u) | (2 * k + 1 < left ? (uint32_t)p[2 * k + 1] : 0u) << 16;
+    } else {
+        const uint32_t* p = (const uint32_t*)base + i;
+        if (left >= N) return *(const LinVec<BF, N>*)p;
 #pragma unroll
-            for (int k = 0; k < N; k++) o[k] = k < left ? __uint_as_float((uint32_t)p[k] << 16) : 0.0f;
+        for (int k = 0; k < N; k++) u.w[k] = k < left ? p[k] : 0u;
+    }
+    return u;
+}
+template <bool BF, int N>
+__device__ __forceinline__ void lin_unpack(const LinVec<BF, N>& u, float* o) {
+    if constexpr (BF) {
+#pragma unroll
+        for (int k = 0; k < N / 2; k++) {
+            o[2 * k] = __uint_as_float(u.w[k] << 16);
+            o[2 * k + 1] = __uint_as_float(u.w[k] & 0xFFFF0000u);
         }
     } else {
-        const float* p = (const float*)base + i;
-        if (left >= N) {
-            const LinRaw<4 * N, 4> u = *(const LinRaw<4 * N, 4>*)p;
 #pragma unroll
-            for (int k = 0; k < N; k++) o[k] = __uint_as_float(u.w[k]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; k++) o[k] = k < left ? p[k] : 0.0f;
-        }
+        for (int k = 0; k < N; k++) o[k] = __uint_as_float(u.w[k]);
     }
+}
+template <bool BF, int N>
+__device__ __forceinline__ void lin_load(const void* base, long long i, int left, float* o) {
+    lin_unpack<BF, N>(lin_get<BF, N>(base, i, left), o);
 }
 template <bool BF, int N>
 __device__ __forceinline__ void lin_store(void* base, long long i, int left, const float* v) {
@@ -253,19 +261,16 @@ __device__ __forceinline__ void lin_rows(const LinEpi& e, int r0, int c0, const 
     // a lane past the last column reads the row's first ones and stores nothing
     const int cc = c < e.ncols ? c : 0, left = e.ncols - cc;
     const bool rd_z = OP == LIN_DGRAD && e.fn != MXC_FN_NONE, rd_s = OP != LIN_WGRAD && e.res;
-    float z[BN][V], s[BN][V], b[V];
-#pragma unroll
-    for (int k = 0; k < BN; k++)
-#pragma unroll
-        for (int q = 0; q < V; q++) z[k][q] = s[k][q] = 0.0f;
+    LinVec<BF, V> z[BN], s[BN];
+    float b[V];
 #pragma unroll
     for (int q = 0; q < V; q++) b[q] = 0.0f;
     auto read = [&](int n) {
 #pragma unroll
         for (int k = 0; k < BN; k++) {
             const int r = min(r0 + row + (n + k) * RS, e.nrows - 1);
-            if (rd_z) lin_load<BF, V>(e.pre, r * e.ldp + cc, left, z[k]);
-            if (rd_s) lin_load<BF, V>(e.res, r * e.ldr + cc, left, s[k]);
+            if (rd_z) z[k] = lin_get<BF, V>(e.pre, r * e.ldp + cc, left);
+            if (rd_s) s[k] = lin_get<BF, V>(e.res, r * e.ldr + cc, left);
         }
     };
     read(0);
@@ -282,13 +287,17 @@ __device__ __forceinline__ void lin_rows(const LinEpi& e, int r0, int c0, const 
 #pragma unroll
             for (int k = 0; k < BN; k++) {
                 const int r = r0 + row + (n + k) * RS;
-                float v[V];
+                float v[V], zf[V], sf[V];
+#pragma unroll
+                for (int q = 0; q < V; q++) zf[q] = sf[q] = 0.0f;
+                if (OP == LIN_DGRAD && decltype(fn)::fn != MXC_FN_NONE) lin_unpack<BF, V>(z[k], zf);
+                if (rd_s) lin_unpack<BF, V>(s[k], sf);
 #pragma unroll
                 for (int q = 0; q < V; q += 4) {
                     const float4 u = *(const float4*)(mine + (row + (n + k) * RS) * LD + col + q);
                     v[q] = u.x; v[q + 1] = u.y; v[q + 2] = u.z; v[q + 3] = u.w;
                 }
-                if (r < e.nrows && c < e.ncols) lin_finish<OP, BF, V, decltype(fn)::fn>(e, r, c, v, b, z[k], s[k]);
+                if (r < e.nrows && c < e.ncols) lin_finish<OP, BF, V, decltype(fn)::fn>(e, r, c, v, b, zf, sf);
             }
         });
     }
@@ -511,6 +520,9 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
         sstep[q] = (uint32_t)(KB * o.scon);
     }
 
+    // held in registers: the address would be loaded again for every stage
+    const uint8_t* zero = g_lin_zero;
+    asm("" : "+s"(zero));
     int kis = kbeg;                               // first contraction block of the next stage to copy
     auto issue = [&](int buf) {
         const uint8_t* lds = smem + buf * L::STAGE;
@@ -526,13 +538,13 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
                 const int slice = q * W + wave;
                 int rb, kb;
                 const bool isb = blk_of(q, rb, kb);
-                dma16_async(kis + kb < kend ? (isb ? bbase : abase) + off[q] : g_lin_zero + lane * 16,
+                dma16_async(kis + kb < kend ? (isb ? bbase : abase) + off[q] : zero + lane * 16,
                             lds_addr(lds + slice * 1024));
             }
         }
 #pragma unroll
         for (int q = 0; q < NSQ; q++) {
-            dma1_async(kis + skb[q] < kend ? sp[q] : g_lin_zero,
+            dma1_async(kis + skb[q] < kend ? sp[q] : zero,
                        lds_addr(lds + L::ABYTES + L::BBYTES + ((q * W + wave) % L::NSI) * 256));
             sp[q] += sstep[q];
         }
