@@ -11,8 +11,6 @@ struct LinPlan {
     long long ldw;                // row length of the partial sums
 };
 
-constexpr int LIN_SPLIT_UNITS = 16;
-
 // nra, nrb: 32-blocks along the output's columns and rows; ncb: along the
 // contraction.  The formats play no part, so neither do they in the workspace.
 LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
@@ -27,10 +25,14 @@ LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
     q.tb = (nrb + q.rb - 1) / q.rb;
     // a grid that leaves CUs idle is split along a long contraction, in units of
     // 16 blocks (a whole number of any shape's stages), four of them a split at
-    // least
+    // least.  The join is a launch of its own: 8 rows x 8192 x 1000 take 10.9 us
+    // whole and 15.7 split, 8 x 16384 x 1000 16 either way; 100 x 8192 x 1000 take
+    // 17 split and 18 whole.  (Splitting grids of one round in two did not pay:
+    // 8192 x 4096 x 1024, both gradients, 84 us whole and 96 split.)
     const long long t = (long long)q.ta * q.tb;
     const int units = (ncb + 15) / 16;
-    const int n = t < 256 && units >= LIN_SPLIT_UNITS ? std::max(1, (int)std::min<long long>(256 / t, units / 4)) : 1;
+    const bool rows = q.tile == LIN_TILE_ROWS32 || q.tile == LIN_TILE_ROWS64;
+    const int n = t < 256 && units >= (rows ? 32 : 16) ? std::max(1, (int)std::min<long long>(256 / t, units / 4)) : 1;
     q.span = (units + n - 1) / n * 16;
     q.nsplit = (ncb + q.span - 1) / q.span;
     q.ldw = (long long)nra * 32;
