@@ -762,7 +762,8 @@ int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void
  * The squares are summed in fp64 in a fixed order; the factor is rounded to
  * fp32, the product is one fp32 operation, rounded once for bf16.  A NaN norm
  * makes the factor NaN, an infinite one makes it 0.  Tensors are contiguous,
- * of n >= 0 elements, fp32 or bf16 each.
+ * of n >= 0 elements, fp32 or bf16 each, and need no more than their elements'
+ * alignment (slices of one buffer).
  *   dst        every tensor's output (its src: in place), or NULL in all of
  *              them: only the norm is formed.  Outputs must not overlap each
  *              other, or a src other than their own.
@@ -771,7 +772,7 @@ int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void
  *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes.
  * The factor is read on the device: no synchronization.  count >= 0; a launch
  * takes 448 tensors, more take several.
- * Errors: NULL, ARG, ALIGN, WORKSPACE, HIP. */
+ * Errors: NULL, ARG, SHAPE (more than 2^40 elements), ALIGN, WORKSPACE, HIP. */
 typedef struct mxc_gtensor {
     const void* src;
     void* dst;

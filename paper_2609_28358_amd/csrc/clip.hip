@@ -39,6 +39,11 @@ __device__ __forceinline__ int find_tensor(const ClipArgs& a, int k) {
     return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
+// 16 bytes at any element's address: global memory takes unaligned vectors.
+struct __attribute__((packed, aligned(2))) Vec16 {
+    uint32_t w[4];
+};
+
 // body(16-byte offset in the chunk) for a workgroup's vectors, four at a time
 // and independent of each other, then tail(first byte, last byte) for what is left
 template <class Body, class Tail>
@@ -61,17 +66,16 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 }
 
 // 16 bytes: 4 fp32 or 8 bf16
-__device__ __forceinline__ double squares(uint4 u, bool bf) {
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+__device__ __forceinline__ double squares(const Vec16& u, bool bf) {
     double s = 0.0;
 #pragma unroll
     for (int k = 0; k < 4; k++) {
         if (bf) {
-            const double lo = __uint_as_float(w[k] << 16), hi = __uint_as_float(w[k] & 0xFFFF0000u);
+            const double lo = __uint_as_float(u.w[k] << 16), hi = __uint_as_float(u.w[k] & 0xFFFF0000u);
             s += lo * lo;
             s += hi * hi;
         } else {
-            const double v = __uint_as_float(w[k]);
+            const double v = __uint_as_float(u.w[k]);
             s += v * v;
         }
     }
@@ -91,9 +95,9 @@ __global__ __launch_bounds__(CT) void clip_norm_kernel(const ClipArgs a, double*
         const int len = (int)min((long long)a.chunk, bytes - b0);
         vectors(len, [&](int o, auto num) {
             constexpr int N = decltype(num)::value;
-            uint4 u[N];
+            Vec16 u[N];
 #pragma unroll
-            for (int i = 0; i < N; i++) u[i] = *(const uint4*)(p + o + i * 16 * CT);
+            for (int i = 0; i < N; i++) u[i] = *(const Vec16*)(p + o + i * 16 * CT);
 #pragma unroll
             for (int i = 0; i < N; i++) s += squares(u[i], bf);
         }, [&](int o, int e) {
@@ -129,18 +133,19 @@ __global__ __launch_bounds__(CT) void clip_scale_kernel(const ClipArgs a, const 
         const int len = (int)min((long long)a.chunk, bytes - b0);
         vectors(len, [&](int o, auto num) {
             constexpr int N = decltype(num)::value;
-            uint4 u[N];
+            Vec16 u[N];
 #pragma unroll
-            for (int i = 0; i < N; i++) u[i] = *(const uint4*)(p + o + i * 16 * CT);
+            for (int i = 0; i < N; i++) u[i] = *(const Vec16*)(p + o + i * 16 * CT);
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
-                uint32_t r[4];
+                Vec16 r;
 #pragma unroll
-                for (int q = 0; q < 4; q++)
-                    r[q] = bf ? bf16_pack2(__uint_as_float(w[q] << 16) * c, __uint_as_float(w[q] & 0xFFFF0000u) * c)
-                              : __float_as_uint(__uint_as_float(w[q]) * c);
-                *(uint4*)(d + o + i * 16 * CT) = make_uint4(r[0], r[1], r[2], r[3]);
+                for (int q = 0; q < 4; q++) {
+                    const uint32_t w = u[i].w[q];
+                    r.w[q] = bf ? bf16_pack2(__uint_as_float(w << 16) * c, __uint_as_float(w & 0xFFFF0000u) * c)
+                                : __float_as_uint(__uint_as_float(w) * c);
+                }
+                *(Vec16*)(d + o + i * 16 * CT) = r;
             }
         }, [&](int o, int e) {
             for (; o < e; o += bf ? 2 : 4) {

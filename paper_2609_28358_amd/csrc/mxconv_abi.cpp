@@ -768,13 +768,15 @@ int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* no
     if (ws_bytes < mxconv_grad_clip_workspace_bytes()) return MXC_ERR_WORKSPACE;
     if (!aligned16(workspace) || !aligned16(norm)) return MXC_ERR_ALIGN;
     int full = -1;                                            // a tensor that is not empty
+    int64_t total = 0;
     for (int i = 0; i < count; i++) {
         if (t[i].n < 0 || t[i].n > (1ll << 36) || (t[i].dtype != MXC_F32 && t[i].dtype != MXC_BF16)) return MXC_ERR_ARG;
         if (!t[i].n) continue;                                // an empty tensor's pointers are not looked at
         if (full < 0) full = i;
         if (!t[i].src) return MXC_ERR_NULL;
         if (!t[i].dst != !t[full].dst) return MXC_ERR_ARG;    // outputs for all tensors or for none
-        if (!aligned16(t[i].src) || !aligned16(t[i].dst)) return MXC_ERR_ALIGN;
+        if ((((uintptr_t)t[i].src | (uintptr_t)t[i].dst) & (t[i].dtype == MXC_BF16 ? 1u : 3u)) != 0) return MXC_ERR_ALIGN;
+        if ((total += t[i].n) > (1ll << 40)) return MXC_ERR_SHAPE;
     }
     const bool scale = full >= 0 && t[full].dst;
     if (!scale && !norm) return full >= 0 ? MXC_ERR_NULL : MXC_OK;   // nothing to write

@@ -52,7 +52,7 @@ SIZES = [(1, 64, 96), (1, 1000, 37), (5, 4500, 70), (31, 32, 33), (47, 260, 300)
          (130, 1, 1), (200, 777, 515), (700, 333, 1030), (1300, 130, 1250),
          (2100, 200, 1990), (1900, 2030, 260),
          # long contractions of each product, split over workgroups
-         (3, 9000, 70), (9000, 40, 70), (40, 70, 9000), (100, 8300, 90)]
+         (3, 17000, 70), (9000, 40, 70), (40, 70, 17000), (100, 8300, 90)]
 
 
 @pytest.mark.parametrize("fmt", list(mm.FORMATS))

@@ -24,9 +24,9 @@ def test_workspace_sizes():
         assert L.mxconv_linear_workspace_bytes(op, _lin()) == 0              # short contractions are not split
     assert L.mxconv_linear_workspace_bytes(2, _lin(9000, 40, 70)) % (40 * 96 * 4) == 0
     assert L.mxconv_linear_workspace_bytes(2, _lin(9000, 40, 70)) > 0
-    assert L.mxconv_linear_workspace_bytes(0, _lin(3, 70, 9000)) > 0
-    assert L.mxconv_linear_workspace_bytes(1, _lin(3, 9000, 70)) > 0
-    assert L.mxconv_linear_workspace_bytes(3, _lin(3, 9000, 70)) == 0
+    assert L.mxconv_linear_workspace_bytes(0, _lin(3, 70, 17000)) > 0
+    assert L.mxconv_linear_workspace_bytes(1, _lin(3, 17000, 70)) > 0
+    assert L.mxconv_linear_workspace_bytes(3, _lin(3, 17000, 70)) == 0
     assert L.mxconv_linear_workspace_bytes(0, _lin(0, 70, 9000)) == 0
     assert L.mxconv_linear_workspace_bytes(0, None) == 0
     assert L.mxconv_grad_clip_workspace_bytes() > 0
@@ -68,7 +68,7 @@ def test_linear_fwd_refusals():
     assert _fwd(z=GOOD, ldz=96) == ARG                                       # z and y are one buffer
     assert _fwd(res=GOOD, ldr=100) == ARG                                    # in place needs one stride
     assert _fwd(bias=ODD) == ALIGN and _fwd(res=ODD, ldr=96) == ALIGN and _fwd(z=ODD, ldz=96) == ALIGN
-    long = _lin(3, 70, 9000)
+    long = _lin(3, 70, 17000)
     need = mx.lib().mxconv_linear_workspace_bytes(0, long)
     assert _fwd(long) == WORKSPACE and _fwd(long, wsp=GOOD, wsb=need - 1) == WORKSPACE
     assert _fwd(long, wsp=ODD, wsb=need) == ALIGN
@@ -166,7 +166,9 @@ def test_clip_refusals():
         assert f(ok, max_norm=m) == ARG
     assert f(ok, tensors=False) == NULL and f(ok, ws=None) == NULL and f(ok, wsb=need - 1) == WORKSPACE
     assert f(ok, ws=ODD) == ALIGN and f(ok, norm=P(0x10004)) == ALIGN
-    assert f((0, 0x20000, 8, 0)) == NULL and f((0x10002, 0x20000, 8, 0)) == ALIGN and f((0x10000, 0x20004, 8, 0)) == ALIGN
+    assert f((0, 0x20000, 8, 0)) == NULL and f((0x10002, 0x20000, 8, 0)) == ALIGN and f((0x10000, 0x20001, 8, 1)) == ALIGN
+    assert f((0x10002, 0x20004, 8, 1), ws=ODD) == ALIGN                      # bf16 at any element is fine, the workspace is not
+    assert f(*[(0x10000 + k, 0, 1 << 36, 0) for k in range(0, 80, 4)]) == SHAPE
     assert f((0x10000, 0x20000, -1, 0)) == ARG and f((0x10000, 0x20000, 8, 2)) == ARG
     assert f(ok, (0x30000, 0, 8, 0)) == ARG                                  # outputs for some tensors only
     assert f((0x10000, 0, 8, 0), norm=None) == NULL                          # nothing to write
