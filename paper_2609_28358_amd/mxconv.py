@@ -604,16 +604,13 @@ def _place(device, stream):
     return None if device.index == here else torch.cuda.device(device)
 
 
-def _placed(fn):
-    """Run a call's launching part, fn(..., device, stream), in its context."""
-    @functools.wraps(fn)
-    def run(*args):
-        place = _place(args[-2], args[-1])
-        if place is None:
-            return fn(*args)
-        with place:
-            return fn(*args)
-    return run
+def _launch(fn, device, stream, *args):
+    """fn(raw stream, *args), a call's launching part, in its context."""
+    place = _place(device, stream)
+    if place is None:
+        return fn(_raw_stream(device.index) if _raw_stream is not None else _stream(None), *args)
+    with place:
+        return fn(_stream(stream), *args)
 
 
 def _rows_cols(t, what, shape, dtype, device):
@@ -654,7 +651,7 @@ def _mx_matrix(q, what):
     c, s = q.codes, q.scales
     dev = c.device
     if (c.dtype != torch.uint8 or s.dtype != torch.uint8 or c.numel() < g[2] or s.numel() < g[3] or
-            not c.is_contiguous() or not s.is_contiguous() or s.device != dev):
+            not (c.is_contiguous() and s.is_contiguous()) or s.get_device() != c.get_device()):
         raise MxconvError(f"{what}: codes and scales must be contiguous uint8 tensors of the matrix's size on one device")
     return g[0], g[1], dev
 
@@ -708,11 +705,10 @@ def linear(w, x, bias=None, fn=FN_NONE, residual=None, dtype=torch.bfloat16, out
         raise MxconvError(f"w is {outs} x {ins} on {wdev}, x {rows} x {k} on {dev}")
     if bias is not None:
         _vector(bias, "bias", (outs,), dev)
-    return _linear((rows, outs), ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace, dev, stream)
+    return _launch(_linear, dev, stream, (rows, outs), ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace, dev)
 
 
-@_placed
-def _linear(shape, ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace, dev, stream):
+def _linear(raw, shape, ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace, dev):
     code = _dtype_code(dtype)
     y = out if out is not None else x.codes.new_empty(shape, dtype=dtype)
     ldr = _rows_cols(residual, "residual", shape, dtype, dev) if residual is not None else 0
@@ -722,7 +718,7 @@ def _linear(shape, ins, w, x, bias, fn, residual, dtype, out, pre_out, workspace
     ws, wp, wb = _workspace(workspace, need[0], dev)
     _check(lib().mxconv_linear_fwd(s, pair(w.fmt, x.fmt), w.codes.data_ptr(), w.scales.data_ptr(), x.codes.data_ptr(),
                                    x.scales.data_ptr(), _ptr(bias), fn, _ptr(residual), ldr, y.data_ptr(), ldy,
-                                   _ptr(pre_out), ldz, code, wp, wb, _stream(stream)), "mxconv_linear_fwd")
+                                   _ptr(pre_out), ldz, code, wp, wb, raw), "mxconv_linear_fwd")
     return y
 
 
@@ -732,11 +728,10 @@ def linear_dgrad(w, dz, fn=FN_NONE, z=None, add=None, dtype=torch.bfloat16, out=
     (outs, ins, wdev), (rows, n, dev) = _mx_matrix(w, "w"), _mx_matrix(dz, "dz")
     if n != outs or wdev != dev:
         raise MxconvError(f"w is {outs} x {ins} on {wdev}, dz {rows} x {n} on {dev}")
-    return _linear_dgrad((rows, ins), outs, w, dz, fn, z, add, dtype, out, workspace, dev, stream)
+    return _launch(_linear_dgrad, dev, stream, (rows, ins), outs, w, dz, fn, z, add, dtype, out, workspace, dev)
 
 
-@_placed
-def _linear_dgrad(shape, outs, w, dz, fn, z, add, dtype, out, workspace, dev, stream):
+def _linear_dgrad(raw, shape, outs, w, dz, fn, z, add, dtype, out, workspace, dev):
     code = _dtype_code(dtype)
     dx = out if out is not None else dz.codes.new_empty(shape, dtype=dtype)
     ldz = _rows_cols(z, "z", shape, dtype, dev) if z is not None else 0
@@ -746,7 +741,7 @@ def _linear_dgrad(shape, outs, w, dz, fn, z, add, dtype, out, workspace, dev, st
     ws, wp, wb = _workspace(workspace, need[1], dev)
     _check(lib().mxconv_linear_dgrad(s, pair(w.fmt, dz.fmt), w.codes.data_ptr(), w.scales.data_ptr(), dz.codes.data_ptr(),
                                      dz.scales.data_ptr(), fn, _ptr(z), ldz, _ptr(add), lda, dx.data_ptr(), ldx, code, wp, wb,
-                                     _stream(stream)), "mxconv_linear_dgrad")
+                                     raw), "mxconv_linear_dgrad")
     return dx
 
 
@@ -757,11 +752,10 @@ def linear_wgrad(dz, x, bias=True, out=None, bias_out=None, workspace=None, stre
     (rows, outs, gdev), (r2, ins, dev) = _mx_matrix(dz, "dz"), _mx_matrix(x, "x")
     if r2 != rows or gdev != dev:
         raise MxconvError(f"dz is {rows} x {outs} on {gdev}, x {r2} x {ins} on {dev}")
-    return _linear_wgrad(rows, outs, ins, dz, x, bias, out, bias_out, workspace, dev, stream)
+    return _launch(_linear_wgrad, dev, stream, rows, outs, ins, dz, x, bias, out, bias_out, workspace, dev)
 
 
-@_placed
-def _linear_wgrad(rows, outs, ins, dz, x, bias, dw, db, workspace, dev, stream):
+def _linear_wgrad(raw, rows, outs, ins, dz, x, bias, dw, db, workspace, dev):
     if dw is None:
         dw = x.codes.new_empty((outs, ins), dtype=torch.float32)
     else:
@@ -773,8 +767,7 @@ def _linear_wgrad(rows, outs, ins, dz, x, bias, dw, db, workspace, dev, stream):
     s, need = _linear_of(rows, outs, ins)
     ws, wp, wb = _workspace(workspace, need[2], dev)
     _check(lib().mxconv_linear_wgrad(s, pair(dz.fmt, x.fmt), dz.codes.data_ptr(), dz.scales.data_ptr(), x.codes.data_ptr(),
-                                     x.scales.data_ptr(), dw.data_ptr(), _ptr(db), wp, wb, _stream(stream)),
-           "mxconv_linear_wgrad")
+                                     x.scales.data_ptr(), dw.data_ptr(), _ptr(db), wp, wb, raw), "mxconv_linear_wgrad")
     return dw, db
 
 
@@ -816,11 +809,10 @@ def norm_residual(x, y, w_post=None, gate=None, scale=1.0, w_pre=None, eps=1e-6,
     fp32 or bf16; w_post, w_pre: fp32 [d] or None (N(y) is y; no U); gate: fp32
     [d], [gates][d] (each for rows / gates consecutive rows) or None."""
     s, gates = _norm_struct(y, w_post, gate, scale, w_pre, eps)
-    return _norm_residual(s, x, y, w_pre is not None, h_out, u_out, y.device, stream)
+    return _launch(_norm_residual, y.device, stream, s, x, y, w_pre is not None, h_out, u_out, y.device)
 
 
-@_placed
-def _norm_residual(s, x, y, pre, h, u, dev, stream):
+def _norm_residual(raw, s, x, y, pre, h, u, dev):
     shape, dt = y.shape, y.dtype
     # a row-major y (checked here): empty_like() is contiguous
     ldx, ldy = _rows_cols(x, "x", shape, dt, dev), _rows_cols(y, "y", shape, dt, dev)
@@ -836,7 +828,7 @@ def _norm_residual(s, x, y, pre, h, u, dev, stream):
     else:
         ldu = _rows_cols(u, "u_out", shape, dt, dev)
     _check(lib().mxconv_norm_fwd(ctypes.byref(s), x.data_ptr(), ldx, y.data_ptr(), ldy, h.data_ptr(), ldh, _ptr(u), ldu,
-                                 _stream(stream)), "mxconv_norm_fwd")
+                                 raw), "mxconv_norm_fwd")
     return h, u
 
 
@@ -851,8 +843,8 @@ def norm_residual_backward(dh, du, h, y, w_post=None, gate=None, scale=1.0, w_pr
         du = h = None
     elif du is None or h is None:
         raise MxconvError("the backward pass of w_pre needs du and h")
-    return _norm_backward(s, gates, dh, du, h, y, w_post is not None, gate is not None, dx_out, dy_out, dw_pre_out, dw_post_out,
-                          dgate_out, workspace, y.device, stream)
+    return _launch(_norm_backward, y.device, stream, s, gates, dh, du, h, y, w_post is not None, gate is not None, dx_out,
+                   dy_out, dw_pre_out, dw_post_out, dgate_out, workspace, y.device)
 
 
 def _result(t, what, shape, dev, like):
@@ -863,8 +855,7 @@ def _result(t, what, shape, dev, like):
     return t
 
 
-@_placed
-def _norm_backward(s, gates, dh, du, h, y, post, gate, dx, dy, dw_pre, dw_post, dgate, workspace, dev, stream):
+def _norm_backward(raw, s, gates, dh, du, h, y, post, gate, dx, dy, dw_pre, dw_post, dgate, workspace, dev):
     shape, dt = y.shape, y.dtype
     rows, d = shape
     lddh, ldy = _rows_cols(dh, "dh", shape, dt, dev), _rows_cols(y, "y", shape, dt, dev)
@@ -885,7 +876,7 @@ def _norm_backward(s, gates, dh, du, h, y, post, gate, dx, dy, dw_pre, dw_post, 
     ws, wp, wb = _workspace(workspace, _norm_workspace_bytes(rows, gates, d, gate, post, h is not None), dev)
     _check(lib().mxconv_norm_bwd(ctypes.byref(s), dh.data_ptr(), lddh, _ptr(du), lddu, _ptr(h), ldh, y.data_ptr(), ldy,
                                  dx.data_ptr(), lddx, dy.data_ptr(), lddy, _ptr(dw_pre), _ptr(dw_post), _ptr(dgate), wp, wb,
-                                 _stream(stream)), "mxconv_norm_bwd")
+                                 raw), "mxconv_norm_bwd")
     return dx, dy, dw_pre, dw_post, dgate
 
 
@@ -925,18 +916,16 @@ def _clip(tensors, outs, max_norm, norm_out, workspace, stream):
         desc[1::4] = array("q", dst)
         if len(set(dst)) != len(dst) and len(set(full := [p for p, n in zip(dst, sizes) if n])) != len(full):
             raise MxconvError("a tensor is written twice")
-    return _clip_launch(len(ptrs), desc, max_norm, norm_out, workspace, dev, stream)
+    return _launch(_clip_launch, dev, stream, len(ptrs), desc, max_norm, norm_out, workspace, dev)
 
 
-@_placed
-def _clip_launch(count, desc, max_norm, norm, workspace, dev, stream):
+def _clip_launch(raw, count, desc, max_norm, norm, workspace, dev):
     if norm is None:
         norm = torch.empty((), dtype=torch.float32, device=dev)
     elif norm.dtype != torch.float32 or norm.numel() != 1 or norm.device != dev:
         raise MxconvError(f"norm_out must be one fp32 element on {dev}")
     ws, wp, wb = _workspace(workspace, _clip_workspace_bytes(), dev)
-    _check(lib().mxconv_grad_clip(count, desc.buffer_info()[0], max_norm, norm.data_ptr(), wp, wb, _stream(stream)),
-           "mxconv_grad_clip")
+    _check(lib().mxconv_grad_clip(count, desc.buffer_info()[0], max_norm, norm.data_ptr(), wp, wb, raw), "mxconv_grad_clip")
     return norm
 
 
