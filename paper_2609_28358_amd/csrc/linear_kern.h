@@ -524,33 +524,36 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
     const uint8_t* zero = g_lin_zero;
     asm("" : "+s"(zero));
     int kis = kbeg;                               // first contraction block of the next stage to copy
-    auto issue = [&](int buf) {
-        const uint8_t* lds = smem + buf * L::STAGE;
-        if (kis + KB <= kend) {
-#pragma unroll
-            for (int q = 0; q < NQ; q++) {
-                const int slice = q * W + wave;
-                dma16_base(slice >= NA ? bbase : abase, off[q], lds_addr(lds + slice * 1024));
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < NQ; q++) {
-                const int slice = q * W + wave;
+    // copy n of the stage's PER (codes, then scales) into the slot at lds; FULL:
+    // every contraction block of the stage exists
+    auto copy = [&](const uint8_t* lds, int n, auto full) {
+        constexpr bool FULL = decltype(full)::value;
+        if (n < NQ) {
+            const int slice = n * W + wave;
+            const bool isb = slice >= NA;
+            if (FULL || kis + KB <= kend) {
+                dma16_base(isb ? bbase : abase, off[n], lds_addr(lds + slice * 1024));
+            } else {
                 int rb, kb;
-                const bool isb = blk_of(q, rb, kb);
-                dma16_async(kis + kb < kend ? (isb ? bbase : abase) + off[q] : zero + lane * 16,
+                blk_of(n, rb, kb);
+                dma16_async(kis + kb < kend ? (isb ? bbase : abase) + off[n] : zero + lane * 16,
                             lds_addr(lds + slice * 1024));
             }
-        }
-#pragma unroll
-        for (int q = 0; q < NSQ; q++) {
-            dma1_async(kis + skb[q] < kend ? sp[q] : zero,
+        } else {
+            const int q = n - NQ;
+            dma1_async((FULL && L::NSI * 64 == (RA + RB) * KB) || kis + skb[q] < kend ? sp[q] : zero,
                        lds_addr(lds + L::ABYTES + L::BBYTES + ((q * W + wave) % L::NSI) * 256));
             sp[q] += sstep[q];
         }
-        abase += astep;
-        bbase += bstep;
-        kis += KB;
+        if (n == PER - 1) {
+            abase += astep;
+            bbase += bstep;
+            kis += KB;
+        }
+    };
+    auto issue = [&](int buf) {
+#pragma unroll
+        for (int n = 0; n < PER; n++) copy(smem + buf * L::STAGE, n, std::false_type{});
     };
 
     const int wk = wave / (WM * WN), wmn = wave - wk * (WM * WN), wm = wmn % WM, wn = wmn / WM;
@@ -597,11 +600,25 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
 #pragma unroll
     for (int i = 0; i < MB; i++) fetch_a(smem, 0, i);
     int buf = 0;
-    for (int st = 0; st < nst; st++) {
+    // One stage.  AHEAD: the copies of stage st + NBUF - 1, a full one, go out
+    // between the products without a branch; else they go out first, where there
+    // are any.
+    auto stage = [&](int st, auto ahead) {
+        constexpr bool AHEAD = decltype(ahead)::value;
         // stage st + 1 is complete for every wave, and stage st - 1's slot is free
-        if (st + 1 < nst) lin_wait<PER>(min(NBUF - 3, nst - 2 - st));
+        if (AHEAD) vm_wait<(NBUF - 3) * PER>();
+        else if (st + 1 < nst) lin_wait<PER>(min(NBUF - 3, nst - 2 - st));
         __syncthreads();
-        if (st + NBUF - 1 < nst) issue(buf == 0 ? NBUF - 1 : buf - 1);
+        const uint8_t* const slot = smem + (buf == 0 ? NBUF - 1 : buf - 1) * L::STAGE;
+        if (!AHEAD && st + NBUF - 1 < nst) issue(buf == 0 ? NBUF - 1 : buf - 1);
+        auto next = [&](int product) {
+            constexpr int PRODUCTS = STEPS * MB * NB, EACH = (PER + PRODUCTS - 1) / PRODUCTS;
+            if constexpr (AHEAD) {
+#pragma unroll
+                for (int n = 0; n < EACH; n++)
+                    if (product * EACH + n < PER) copy(slot, product * EACH + n, std::true_type{});
+            }
+        };
         const uint8_t* cur = smem + buf * L::STAGE;
         buf = buf + 1 == NBUF ? 0 : buf + 1;
         // past the last stage the ring's old bytes are read and not used
@@ -626,17 +643,27 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
                     e4m3_decode32(rawa[i], sca[i][0], sca[i][1], da);
                     fetch_a(ns, n, i);
 #pragma unroll
-                    for (int j = 0; j < NB; j++) acc[i][j] = mfma_x8(da, db[j], acc[i][j]);
+                    for (int j = 0; j < NB; j++) {
+                        acc[i][j] = mfma_x8(da, db[j], acc[i][j]);
+                        next((s * MB + i) * NB + j);
+                    }
                 } else {
                     const v8i fa = rawa[i];
                     const int sa = sca[i][0];
                     fetch_a(ns, n, i);
 #pragma unroll
-                    for (int j = 0; j < NB; j++) acc[i][j] = mfma_mx<FA, FB>(fa, fb[j], acc[i][j], sa, sb[j]);
+                    for (int j = 0; j < NB; j++) {
+                        acc[i][j] = mfma_mx<FA, FB>(fa, fb[j], acc[i][j], sa, sb[j]);
+                        next((s * MB + i) * NB + j);
+                    }
                 }
             }
         }
-    }
+    };
+    const int nahead = max(0, (kend - kbeg) / KB - (NBUF - 1));      // stages whose copies are of a full one
+    int st0 = 0;
+    for (; st0 < nahead; st0++) stage(st0, std::true_type{});
+    for (; st0 < nst; st0++) stage(st0, std::false_type{});
 
     // ---- write: lane l holds output row l % 32 of B's block and, in quad q,
     // columns 8 q + 4 (l / 32) .. + 3 of A's block

@@ -14,12 +14,12 @@ template <int FA, int FB> constexpr int lin_ks() { return FA == MXC_E2M1 && FB =
 // The shapes that linear.hip's plan chooses among (LIN_TILE_*).
 template <int FA, int FB, int OP>
 int linear_launch_op(const LinArgs& a, int tile, hipStream_t s) {
-    constexpr int KS = lin_ks<FA, FB>();
+    constexpr int KS = lin_ks<FA, FB>(), N64 = KS == 4 ? 4 : 3;
     if constexpr (OP != LIN_WGRAD) {
         if (tile == LIN_TILE_ROWS32) return linear_launch<FA, FB, OP, LinTile<1, 1, 1, 1, 8, 2, 4>>(a, s);
         if (tile == LIN_TILE_ROWS64) return linear_launch<FA, FB, OP, LinTile<1, 2, 1, 1, 8, 2, 3>>(a, s);
     }
-    if (tile == LIN_TILE_64) return linear_launch<FA, FB, OP, LinTile<1, 1, 2, 2, 1, 2 * KS, 4>>(a, s);
+    if (tile == LIN_TILE_64) return linear_launch<FA, FB, OP, LinTile<1, 1, 2, 2, 1, 4, N64>>(a, s);
     if (tile == LIN_TILE_128) return linear_launch<FA, FB, OP, LinTile<2, 2, 2, 2, 1, KS, 4>>(a, s);
     return linear_launch<FA, FB, OP, LinTile<4, 2, 2, 2, 1, KS, 3>>(a, s);
 }
