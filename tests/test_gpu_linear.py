@@ -149,6 +149,54 @@ def test_gradient_against_differences(mx):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_results_larger_than_the_caches(mx, dtype):
+    """Whole-line rows of a result past 32 MB are stored past the caches; the
+    same product with rows that begin elsewhere gives the same values."""
+    rows, ins, outs = 8200, 64, 2048
+    x, xv = mm.matrix(mx, rows, ins, 1, 5)
+    w, wv = mm.matrix(mx, outs, ins, 1, 6)
+    res = _rand((rows, outs), 7, dtype)
+    pre = torch.empty((rows, outs), dtype=dtype, device=DEV)
+    y = mx.linear(w, x, fn=2, residual=res, dtype=dtype, pre_out=pre)
+    z, tz, yr, ty = _fwd_ref(xv, wv, None, 2, res)
+    mm.check(pre, z, tz, dtype, "pre")
+    mm.check(y, yr, ty, dtype, "y")
+    wide = torch.full((rows, outs + 8), 9.0, dtype=dtype, device=DEV)
+    mx.linear(w, x, fn=2, residual=res, dtype=dtype, out=wide[:, :outs])
+    assert torch.equal(wide[:, :outs], y) and (wide[:, outs:] == 9).all()
+    dz, gv = mm.matrix(mx, rows, 64, 1, 8)
+    w2, w2v = mm.matrix(mx, 64, outs, 1, 9)
+    dx = mx.linear_dgrad(w2, dz, fn=1, z=pre, dtype=dtype)
+    ref, tol = gv @ w2v, mm.product_tol(gv, w2v.T)
+    on = _np(pre) > 0
+    mm.check(dx, ref * on, tol * on, dtype, "dx")
+
+
+def test_calls_from_two_threads(mx):
+    """Concurrent calls on streams of their own equal the sequential ones."""
+    import threading
+    x, _ = mm.matrix(mx, 9000, 200, 1, 1)
+    dz, _ = mm.matrix(mx, 9000, 96, 1, 2)
+    w, _ = mm.matrix(mx, 96, 200, 1, 3)
+    want = (mx.linear(w, x), *mx.linear_wgrad(dz, x))
+    torch.cuda.synchronize()
+    got, streams = [None, None], [torch.cuda.Stream() for _ in range(2)]
+
+    def work(k):
+        for _ in range(10):
+            got[k] = (mx.linear(w, x, stream=streams[k]), *mx.linear_wgrad(dz, x, stream=streams[k]))
+        streams[k].synchronize()
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("pad", [1, 4, 13])
 def test_strided_rows_and_untouched_columns(mx, dtype, pad):
     """Outputs, residual and pre-activation as column ranges of wider buffers:
