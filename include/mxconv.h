@@ -665,7 +665,8 @@ int mxconv_quantize_sum_sr(int fmt, int n, int c, int h, int w, int nterms, cons
  * `dtype` (fp32, or bf16 to nearest even).  Full-precision matrices are
  * row-major with unit column stride and the given row stride in elements (at
  * least the number of columns, any remainder); pointers are 16-byte aligned.
- * rows >= 1; outs and ins at most MXC_LINEAR_MAX_DIM.
+ * rows at most MXC_LINEAR_MAX_ROWS, outs and ins at most MXC_LINEAR_MAX_DIM, each
+ * at least 1.
  *
  * Forward:  Y = fn(Z) + residual.
  *   bias      NULL, or device fp32 [outs].
@@ -687,6 +688,7 @@ int mxconv_quantize_sum_sr(int fmt, int n, int c, int h, int w, int nterms, cons
  * Errors: NULL, ARG (enum, sizes, strides), SHAPE (a matrix too large),
  * ALIGN, WORKSPACE, HIP. */
 #define MXC_LINEAR_MAX_DIM (1 << 20)
+#define MXC_LINEAR_MAX_ROWS (1 << 30)
 typedef enum { MXC_LINEAR_FWD = 0, MXC_LINEAR_DGRAD = 1, MXC_LINEAR_WGRAD = 2 } mxc_linear_op;
 typedef struct mxc_linear {
     int32_t rows, outs, ins;

@@ -613,7 +613,7 @@ static int linear_fmts(int fmt, int* f1, int* f2) {
 
 static int linear_check(const mxc_linear* p) {
     if (p->rows <= 0 || p->outs <= 0 || p->ins <= 0) return MXC_ERR_ARG;
-    if (p->outs > MXC_LINEAR_MAX_DIM || p->ins > MXC_LINEAR_MAX_DIM) return MXC_ERR_SHAPE;
+    if (p->rows > MXC_LINEAR_MAX_ROWS || p->outs > MXC_LINEAR_MAX_DIM || p->ins > MXC_LINEAR_MAX_DIM) return MXC_ERR_SHAPE;
     Geom g;     // the stored matrices' own limits
     int rc;
     if ((rc = geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->rows, p->ins, 1, 1))) return rc;

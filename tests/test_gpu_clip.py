@@ -141,47 +141,6 @@ def test_duplicates_and_mismatches_are_refused(mx):
     assert abs(float(mx.grad_norm([a, a])) - 4.0) < 1e-6
 
 
-@pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
-def test_any_element_alignment(mx, dtype):
-    """Slices that begin at every element offset of a 16-byte vector, with
-    lengths around vectors and chunks: the results of aligned copies, and
-    the elements between the slices as they were."""
-    g = torch.Generator()
-    g.manual_seed(3)
-    src = torch.randn(60000, generator=g).to(dtype).to(DEV)
-    dst = torch.full((60000,), 7.0, dtype=dtype, device=DEV)
-    cuts, at = [], 1
-    for n in (1, 5, 16, 31, 4096, 4097, 8200, 100, 13, 9001):
-        cuts.append((at, n))
-        at += n + 2
-    ins, outs = [src[a:a + n] for a, n in cuts], [dst[a:a + n] for a, n in cuts]
-    assert len({t.data_ptr() % 16 for t in ins}) > 3
-    norm = mx.grad_clip(ins, 1.0, out=outs)
-    want = [torch.empty_like(t) for t in ins]
-    assert float(mx.grad_clip([t.clone() for t in ins], 1.0, out=want)) == float(norm)
-    keep = torch.ones(60000, dtype=torch.bool, device=DEV)
-    for (a, n), o, w in zip(cuts, outs, want):
-        assert torch.equal(o, w)
-        keep[a:a + n] = False
-    assert (dst[keep] == 7).all()
-
-
-def test_duplicates_and_mismatches_are_refused(mx):
-    a, b = torch.ones(8, device=DEV), torch.ones(8, device=DEV)
-    for call in (lambda: mx.grad_clip([a, a], 1.0), lambda: mx.grad_clip([a, b], 1.0, out=[b, b]),
-                 lambda: mx.grad_clip([a, b], 1.0, out=[a]), lambda: mx.grad_clip([a], 1.0, out=[torch.ones(7, device=DEV)]),
-                 lambda: mx.grad_clip([a, b.bfloat16()], 1.0, out=[a, b]), lambda: mx.grad_clip([a.view(2, 4).t()], 1.0),
-                 lambda: mx.grad_clip([a.half()], 1.0), lambda: mx.grad_clip([a, b.cpu()], 1.0),
-                 lambda: mx.grad_clip([a], float("nan")), lambda: mx.grad_clip([a], -1.0),
-                 lambda: mx.grad_clip([a], 1.0, norm_out=torch.zeros(2, device=DEV)),
-                 lambda: mx.grad_clip([a], 1.0, workspace=torch.zeros(8, dtype=torch.uint8, device=DEV))):
-        with pytest.raises(mx.MxconvError):
-            call()
-    assert (a == 1).all() and (b == 1).all()
-    # reading one twice is fine: both count
-    assert abs(float(mx.grad_norm([a, a])) - 4.0) < 1e-6
-
-
 def test_graph_replay_reads_new_gradients(mx):
     ts = _make([5000, 7, 130], [F, B], 1.0)
     outs = [torch.empty_like(t) for t in ts]

@@ -104,6 +104,18 @@ def test_linear_wgrad_refusals():
     assert f(_lin(9000, 40, 70)) == WORKSPACE
 
 
+def test_rows_near_the_integer_limit():
+    """Rows whose rounding up to blocks would pass 31 bits are refused by every
+    product, also where they are only the contraction."""
+    L = mx.lib()
+    for rows in ((1 << 30) + 1, 2 ** 31 - 33, 2 ** 31 - 31, 2 ** 31 - 1):
+        lin = _lin(rows, 32, 32)
+        assert [L.mxconv_linear_workspace_bytes(op, lin) for op in range(3)] == [0, 0, 0]
+        assert L.mxconv_linear_fwd(lin, 1, GOOD, GOOD, GOOD, GOOD, None, 0, None, 0, GOOD, 32, None, 0, 0, None, 0, None) == SHAPE
+        assert L.mxconv_linear_dgrad(lin, 1, GOOD, GOOD, GOOD, GOOD, 0, None, 0, None, 0, GOOD, 32, 0, None, 0, None) == SHAPE
+        assert L.mxconv_linear_wgrad(lin, 1, GOOD, GOOD, GOOD, GOOD, GOOD, None, GOOD, 1 << 40, None) == SHAPE
+
+
 def _norm(rows=10, gates=2, d=48, dtype=0, eps=1e-6, post=GOOD, gate=GOOD, pre=GOOD):
     return ctypes.byref(mx.MxcNorm(rows, gates, d, dtype, 1.0, eps, post, gate, pre))
 
