@@ -664,7 +664,9 @@ int mxconv_quantize_sum_sr(int fmt, int n, int c, int h, int w, int nterms, cons
  * fp32, everything in the epilogue is fp32, and a result is rounded once, to
  * `dtype` (fp32, or bf16 to nearest even).  Full-precision matrices are
  * row-major with unit column stride and the given row stride in elements (at
- * least the number of columns, any remainder); pointers are 16-byte aligned.
+ * least the number of columns, any remainder), and they and the vectors need no
+ * more than their elements' alignment; codes, scales and the workspace are
+ * 16-byte aligned.
  * rows at most MXC_LINEAR_MAX_ROWS, outs and ins at most MXC_LINEAR_MAX_DIM, each
  * at least 1.
  *
@@ -719,7 +721,8 @@ int mxconv_linear_wgrad(const mxc_linear* lin, int fmt,
  *   N(v; w) = w . v / sqrt(mean(v^2) + eps) over a row of d values.
  * All arithmetic is fp32; H and U are rounded once, and U is formed from the
  * unrounded H.  Row-major matrices of `dtype` (fp32 or bf16), unit column
- * stride and a row stride in elements (>= d).
+ * stride and a row stride in elements (>= d); nothing but the workspace (16
+ * bytes) needs more than its elements' alignment.
  *   w_post  NULL (N(Y) is then Y itself), or device fp32 [d];
  *   gate    NULL (1), or device fp32 [gates][d]: row r has gate r / (rows /
  *           gates); gates divides rows (one gate for all rows: gates = 1);
@@ -763,15 +766,16 @@ int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void
  *   norm = sqrt(sum g^2),  dst = g * min(1, max_norm / (norm + 1e-6)).
  * The squares are summed in fp64 in a fixed order; the factor is rounded to
  * fp32, the product is one fp32 operation, rounded once for bf16.  A NaN norm
- * makes the factor NaN, an infinite one makes it 0.  Tensors are contiguous,
+ * makes the factor NaN, an infinite one makes it 0 (NaN if max_norm is infinite
+ * too).  Tensors are contiguous,
  * of n >= 0 elements, fp32 or bf16 each, and need no more than their elements'
  * alignment (slices of one buffer).
  *   dst        every tensor's output (its src: in place), or NULL in all of
  *              them: only the norm is formed.  Outputs must not overlap each
  *              other, or a src other than their own.
- *   max_norm   >= 0 (infinity: never scaled).
+ *   max_norm   >= 0 (infinity: a finite norm is never scaled).
  *   norm       NULL, or device fp32 [1], written (0 for no elements).
- *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes.
+ *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes, 16-byte aligned.
  * The factor is read on the device: no synchronization.  count >= 0; a launch
  * takes 448 tensors, more take several.
  * Errors: NULL, ARG, SHAPE (more than 2^40 elements), ALIGN, WORKSPACE, HIP. */

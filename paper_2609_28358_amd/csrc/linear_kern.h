@@ -435,8 +435,8 @@ __device__ __forceinline__ void lin_colsum(const LinOp& o, float* out, int n, in
 // A workgroup computes RA x RB blocks of 32 x 32 outputs.  A stage holds KB
 // contraction blocks of both operands, copied to LDS by global -> LDS loads
 // into a ring of NBUF stages: while one is multiplied the next is complete and
-// the two after it are in flight; one barrier a stage publishes the next and
-// frees the one before.
+// the NBUF - 2 after it are in flight, issued between the products; one barrier
+// a stage publishes the next and frees the one before.
 // Row blocks past the end read the last one (their products are not stored);
 // contraction blocks past the end read zero codes and scales.
 template <int FA, int FB, int OP, class T>

@@ -602,6 +602,9 @@ int mxconv_naive_wgrad(const mxc_conv* p, int fmt, const void* gtc, const uint8_
     return launch_naive_wgrad(cv, gtc, gts, xtc, xts, gw, (hipStream_t)stream);
 }
 
+// Full-precision operands of the calls below need their elements' alignment.
+static bool aligned_to(int dtype, const void* p) { return ((uintptr_t)p & (dtype == MXC_BF16 ? 1 : 3)) == 0; }
+
 // ---- linear layers
 // The formats of a linear product's operands (in the call's order).
 static int linear_fmts(int fmt, int* f1, int* f2) {
@@ -637,9 +640,10 @@ static int linear_run(int op, const mxc_linear& p, int fa, int fb, const LinMat&
     linear_dims(op, p, &e.nrows, &e.ncols, &ncon);
     const size_t need = linear_workspace(op, e.nrows, e.ncols, ncon);
     if (need && (!ws || ws_bytes < need)) return MXC_ERR_WORKSPACE;
+    const int dt = e.bf16 ? MXC_BF16 : MXC_F32;
     if (!aligned16(a.codes) || !aligned16(a.scales) || !aligned16(b.codes) || !aligned16(b.scales) ||
-        !aligned16(e.out) || !aligned16(e.res) || !aligned16(e.pre) || !aligned16(e.bias) || !aligned16(colsum) ||
-        (need && !aligned16(ws)))
+        !aligned_to(dt, e.out) || !aligned_to(dt, e.res) || !aligned_to(dt, e.pre) || !aligned_to(MXC_F32, e.bias) ||
+        !aligned_to(MXC_F32, colsum) || (need && !aligned16(ws)))
         return MXC_ERR_ALIGN;
     const int es = e.bf16 ? 2 : 4;
     const bool written = op != LIN_DGRAD && e.pre;            // a second result (the input gradient only reads it)
@@ -705,6 +709,10 @@ static int norm_check(const mxc_norm* p) {
     return MXC_OK;
 }
 
+static bool norm_params_aligned(const mxc_norm& p) {
+    return aligned_to(MXC_F32, p.w_post) && aligned_to(MXC_F32, p.gate) && aligned_to(MXC_F32, p.w_pre);
+}
+
 static NormArgs norm_args(const mxc_norm& p) {
     NormArgs a = {};
     a.w_post = p.w_post; a.w_pre = p.w_pre; a.gate = p.gate;
@@ -724,9 +732,9 @@ int mxconv_norm_fwd(const mxc_norm* p, const void* x, int64_t ldx, const void* y
     if (!p->w_pre) { u = nullptr; ldu = p->d; }
     if (ldx < p->d || ldy < p->d || ldh < p->d || ldu < p->d) return MXC_ERR_ARG;
     if (u == h || (h == x && ldh != ldx)) return MXC_ERR_ARG;
-    if (!aligned16(x) || !aligned16(y) || !aligned16(h) || !aligned16(u) || !aligned16(p->w_post) ||
-        !aligned16(p->gate) || !aligned16(p->w_pre))
-        return MXC_ERR_ALIGN;
+    for (const void* q : {x, y, (const void*)h, (const void*)u})
+        if (!aligned_to(p->dtype, q)) return MXC_ERR_ALIGN;
+    if (!norm_params_aligned(*p)) return MXC_ERR_ALIGN;
     NormArgs a = norm_args(*p);
     a.x = x; a.y = y; a.h = h; a.u = u;
     a.ldx = ldx; a.ldy = ldy; a.ldh = ldh; a.ldu = ldu;
@@ -751,10 +759,11 @@ int mxconv_norm_bwd(const mxc_norm* p, const void* dh, int64_t lddh, const void*
     if (dx == dy || (dx == dh && lddx != lddh) || (dy == y && lddy != ldy)) return MXC_ERR_ARG;
     const size_t need = mxconv_norm_workspace_bytes(p);
     if (need && (!workspace || ws_bytes < need)) return MXC_ERR_WORKSPACE;
-    if (!aligned16(dh) || !aligned16(du) || !aligned16(h) || !aligned16(y) || !aligned16(dx) || !aligned16(dy) ||
-        !aligned16(p->w_post) || !aligned16(p->gate) || !aligned16(p->w_pre) || !aligned16(dw_pre) ||
-        !aligned16(dw_post) || !aligned16(dgate) || (need && !aligned16(workspace)))
-        return MXC_ERR_ALIGN;
+    for (const void* q : {dh, du, h, y, (const void*)dx, (const void*)dy})
+        if (!aligned_to(p->dtype, q)) return MXC_ERR_ALIGN;
+    for (const float* q : {dw_pre, dw_post, dgate})
+        if (!aligned_to(MXC_F32, q)) return MXC_ERR_ALIGN;
+    if (!norm_params_aligned(*p) || (need && !aligned16(workspace))) return MXC_ERR_ALIGN;
     NormArgs a = norm_args(*p);
     a.x = dh; a.y = y; a.h = const_cast<void*>(h); a.u = const_cast<void*>(du);
     a.dx = dx; a.dy = dy;
@@ -770,7 +779,7 @@ int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* no
     if (count < 0 || count > MXC_CLIP_MAX || !(max_norm >= 0.0)) return MXC_ERR_ARG;
     if ((count > 0 && !t) || !workspace) return MXC_ERR_NULL;
     if (ws_bytes < mxconv_grad_clip_workspace_bytes()) return MXC_ERR_WORKSPACE;
-    if (!aligned16(workspace) || !aligned16(norm)) return MXC_ERR_ALIGN;
+    if (!aligned16(workspace) || !aligned_to(MXC_F32, norm)) return MXC_ERR_ALIGN;
     int full = -1;                                            // a tensor that is not empty
     int64_t total = 0;
     for (int i = 0; i < count; i++) {
@@ -779,7 +788,7 @@ int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* no
         if (full < 0) full = i;
         if (!t[i].src) return MXC_ERR_NULL;
         if (!t[i].dst != !t[full].dst) return MXC_ERR_ARG;    // outputs for all tensors or for none
-        if ((((uintptr_t)t[i].src | (uintptr_t)t[i].dst) & (t[i].dtype == MXC_BF16 ? 1u : 3u)) != 0) return MXC_ERR_ALIGN;
+        if (!aligned_to(t[i].dtype, t[i].src) || !aligned_to(t[i].dtype, t[i].dst)) return MXC_ERR_ALIGN;
         if ((total += t[i].n) > (1ll << 40)) return MXC_ERR_SHAPE;
     }
     const bool scale = full >= 0 && t[full].dst;
@@ -795,7 +804,8 @@ const char* mxconv_strerror(int code) {
         case MXC_ERR_SHAPE: return "unsupported shape (batch must divide 32 or be a multiple of 32; "
                                    "E2M1 needs at least 2 samples per block, FP6 at least 4; output must be non-empty; "
                                    "FP6 GEMMs need batch block 32 and the lean kernels' shapes)";
-        case MXC_ERR_ALIGN: return "device pointer not 16-byte aligned";
+        case MXC_ERR_ALIGN: return "device pointer not aligned (16 bytes; full-precision operands of linear layers, residual "
+                                   "norms and gradient clipping: their elements)";
         case MXC_ERR_HIP: return "HIP launch error";
         case MXC_ERR_WORKSPACE: return "workspace missing or too small";
         default: return "unknown error";

@@ -161,3 +161,24 @@ def test_graph_replay_reads_new_gradients(mx):
         want = [torch.empty_like(t) for t in ts]
         assert float(mx.grad_clip(ts, 1.0, out=want)) == got
         assert all(torch.equal(a, b) for a, b in zip(vals, want))
+
+
+def test_norms_kept_in_one_log(mx):
+    """norm_out may be any element of a buffer; its neighbours stay."""
+    ts = _make([500, 33], [F, B], 1.0)
+    log = torch.full((6,), -1.0, device=DEV)
+    want = float(mx.grad_norm(ts))
+    for k in (1, 3, 4):
+        mx.grad_clip(ts, 1e9, norm_out=log[k])
+    assert log.tolist() == [-1.0, want, -1.0, want, want, -1.0]
+
+
+def test_infinite_bound(mx):
+    """Never scaled; only with an infinite norm the factor is inf / inf."""
+    ts = _make([500, 33], [F, B], 1.0)
+    outs = [torch.empty_like(t) for t in ts]
+    mx.grad_clip(ts, float("inf"), out=outs)
+    assert all(torch.equal(a, b) for a, b in zip(ts, outs))
+    ts[1][0] = float("inf")
+    assert float(mx.grad_clip(ts, float("inf"), out=outs)) == float("inf")
+    assert all(torch.isnan(o).all() for o in outs)

@@ -303,3 +303,42 @@ def test_stream_and_graph(mx):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), k
         step()
+
+
+def _at(t, k, fill=9.0):
+    """(buffer, its view of t's shape k elements in)"""
+    buf = torch.full((t.numel() + 16,), fill, dtype=t.dtype, device=t.device)
+    v = buf[k:k + t.numel()].view(t.shape)
+    return buf, v
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size", [(3, 96, 70), (130, 96, 200), (3, 17000, 70)], ids=lambda s: "x".join(map(str, s)))
+def test_pointers_at_any_element(mx, dtype, size):
+    """Full-precision operands that begin at odd elements: the bits of aligned
+    ones, and nothing written around them."""
+    rows, ins, outs = size
+    x, _ = mm.matrix(mx, rows, ins, 0, 1)
+    w, _ = mm.matrix(mx, outs, ins, 0, 2, std=ins ** -0.5)
+    dz, _ = mm.matrix(mx, rows, outs, 0, 3)
+    bias, res = _rand((outs,), 4, torch.float32), _rand((rows, outs), 5, dtype)
+    z, add = _rand((rows, ins), 6, dtype), _rand((rows, ins), 7, dtype)
+    pre = torch.empty_like(res)
+    y = mx.linear(w, x, bias=bias, fn=2, residual=res, dtype=dtype, pre_out=pre)
+    dx = mx.linear_dgrad(w, dz, fn=2, z=z, add=add, dtype=dtype)
+    dw, db = mx.linear_wgrad(dz, x)
+
+    def put(t, k):
+        buf, v = _at(t, k)
+        v.copy_(t)
+        return v
+
+    for k in (1, 3):
+        bufs = [_at(t, k) for t in (y, pre, dx, dw, db)]
+        o = [v for _, v in bufs]
+        mx.linear(w, x, bias=put(bias, k), fn=2, residual=put(res, k + 1), dtype=dtype, out=o[0], pre_out=o[1])
+        mx.linear_dgrad(w, dz, fn=2, z=put(z, k + 4), add=put(add, k), dtype=dtype, out=o[2])
+        mx.linear_wgrad(dz, x, out=o[3], bias_out=o[4])
+        for name, ref, (buf, v) in zip(("y", "pre", "dx", "dw", "db"), (y, pre, dx, dw, db), bufs):
+            assert torch.equal(v, ref), name
+            assert (buf[:k] == 9).all() and (buf[k + ref.numel():] == 9).all(), name

@@ -121,9 +121,10 @@ def _bwd_ref(dh, du, h, y, wp, wq, g, s):
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}x{c[1]}g{c[2]}{'p' if c[3] else ''}{'q' if c[4] else ''}")
 def test_backward(mx, dtype, case):
-    """The column sums' bound adds one rounding a row in a run and a run in
-    the join, at most rows / 1024 + 8 + 32 + 1024 / 8: within 3 C = 96 plus the
-    64 below at these sizes (at most 3 rows a run, 128 partial rows a thread)."""
+    """The column sums' bound adds one rounding a row that a thread takes (at
+    most 3000 / 256 + 1), one for each of a workgroup's up to 8 rows at a time,
+    512 / 32 in a thread of the join and 32 over its threads: 69, within the
+    160 below."""
     rows, d = case[:2]
     seed = 100 * CASES.index(case) + 50
     h, y, wp, wq, g = _case(case, dtype, seed)
@@ -242,3 +243,42 @@ def test_graph_replay(mx):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), k
         step()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [37, 1030])
+def test_pointers_at_any_element(mx, dtype, d):
+    """Operands, parameters and results that begin at odd elements: the bits of
+    aligned ones, and nothing written around them."""
+    rows = 24
+    case = (rows, d, 3, True, True)
+    x, y, wp, wq, g = _case(case, dtype, 900)
+    dh, du = _rand((rows, d), 910, dtype), _rand((rows, d), 911, dtype)
+    kw = dict(scale=0.7, eps=EPS)
+    h, u = mx.norm_residual(x, y, w_post=wp, gate=g, w_pre=wq, **kw)
+    grads = mx.norm_residual_backward(dh, du, h, y, w_post=wp, gate=g, w_pre=wq, **kw)
+
+    def at(t, k):
+        buf = torch.full((t.numel() + 16,), 9.0, dtype=t.dtype, device=DEV)
+        return buf, buf[k:k + t.numel()].view(t.shape)
+
+    def put(t, k):
+        v = at(t, k)[1]
+        v.copy_(t)
+        return v
+
+    def same(ref, bufs, k):
+        for t, (buf, v) in zip(ref, bufs):
+            assert torch.equal(t, v)
+            assert (buf[:k] == 9).all() and (buf[k + t.numel():] == 9).all()
+
+    for k in (1, 3):
+        p = dict(w_post=put(wp, k), gate=put(g, k + 1), w_pre=put(wq, k + 2), **kw)
+        outs = [at(t, k) for t in (h, u)]
+        mx.norm_residual(put(x, k), put(y, k + 1), h_out=outs[0][1], u_out=outs[1][1], **p)
+        same((h, u), outs, k)
+        bufs = [at(t, k) for t in grads]
+        o = [v for _, v in bufs]
+        mx.norm_residual_backward(put(dh, k), put(du, k + 1), put(h, k + 2), put(y, k), dx_out=o[0], dy_out=o[1],
+                                  dw_pre_out=o[2], dw_post_out=o[3], dgate_out=o[4], **p)
+        same(grads, bufs, k)

@@ -74,6 +74,21 @@ def test_linear_fwd_refusals():
     assert _fwd(long, wsp=ODD, wsb=need) == ALIGN
 
 
+def test_elements_alignment_is_enough():
+    """What is checked last for each call is the workspace: full-precision
+    operands at any element get that far."""
+    long, big = _lin(3, 70, 17000), _norm(rows=5000)
+    need = mx.lib().mxconv_linear_workspace_bytes(0, long)
+    f4, h2 = P(0x10004), P(0x30002)
+    for dtype, a, b in ((0, f4, P(0x20008)), (1, h2, P(0x40006))):
+        kw = dict(y=a, ldy=96, bias=f4, res=b, ldr=96, z=P(b.value + 0x1000), ldz=96, dtype=dtype)
+        assert _fwd(long, wsp=ODD, wsb=need, **kw) == ALIGN
+        assert _fwd(long, wsp=GOOD, wsb=need - 1, **kw) == WORKSPACE
+    assert _fwd(y=h2, dtype=0) == ALIGN and _fwd(bias=h2, dtype=1) == ALIGN
+    assert mx.lib().mxconv_norm_fwd(_norm(gate=h2), GOOD, 48, GOOD, 48, GOOD, 48, P(0x20000), 48, None) == ALIGN
+    assert mx.lib().mxconv_norm_fwd(_norm(), h2, 48, GOOD, 48, GOOD, 48, P(0x20000), 48, None) == ALIGN
+
+
 def test_linear_dgrad_refusals():
     L = mx.lib()
 
@@ -177,7 +192,7 @@ def test_clip_refusals():
     for m in (-1.0, float("nan")):
         assert f(ok, max_norm=m) == ARG
     assert f(ok, tensors=False) == NULL and f(ok, ws=None) == NULL and f(ok, wsb=need - 1) == WORKSPACE
-    assert f(ok, ws=ODD) == ALIGN and f(ok, norm=P(0x10004)) == ALIGN
+    assert f(ok, ws=ODD) == ALIGN and f(ok, norm=P(0x10002)) == ALIGN
     assert f((0, 0x20000, 8, 0)) == NULL and f((0x10002, 0x20000, 8, 0)) == ALIGN and f((0x10000, 0x20001, 8, 1)) == ALIGN
     assert f((0x10002, 0x20004, 8, 1), ws=ODD) == ALIGN                      # bf16 at any element is fine, the workspace is not
     assert f(*[(0x10000 + k, 0, 1 << 36, 0) for k in range(0, 80, 4)]) == SHAPE
