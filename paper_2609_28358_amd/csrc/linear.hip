@@ -13,6 +13,20 @@ struct LinPlan {
 
 // nra, nrb: 32-blocks along the output's columns and rows; ncb: along the
 // contraction.  The formats play no part, so neither do they in the workspace.
+// Larger tiles read less, smaller ones fill more CUs.  Measured on both sides of
+// each limit (forward, us, MXFP8 / MXFP4; rows x outs x ins):
+//   32 rows or fewer, 64 or fewer: one tile takes them all and its waves share the
+//     contraction.  32 x 4096 x 4096 7.9 / 5.9 against 18.7 / 10.6 by 64 x 64
+//     tiles, 64 x 4096 x 4096 10.0 / 6.9 against 18.8 / 10.6;
+//   two 256 x 128 tiles a CU: 4096 x 4096 x 1024 42.9 / 26.4 against 44.3 / 26.8
+//     by 128 x 128 ones; with one a CU (2048 x 4096 x 1024) 27.2 / 18.6 against
+//     24.3 / 13.9;
+//   one 128 x 128 tile a CU: 2048 x 2048 x 1024 15.4 / 9.6 against 17.8 / 10.6 by
+//     64 x 64 ones; half as many (1024 x 2048 x 1024) 13.9 / 9.6 against 10.7 / 7.2;
+//   at most one 64 x 64 tile a CU and 40 blocks to contract: its waves share the
+//     contraction, two to a SIMD.  128 x 8192 x 8192 27.5 / 14.6 against 40.3 /
+//     18.5 by four waves with a quarter of the tile each, 1024 x 544 x 1504 8.9 /
+//     6.8 against 9.7 / 6.7; 800 x 1120 x 1024 7.9 / 6.4 against 7.9 / 6.0.
 LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
     LinPlan q;
     auto tiles = [&](int a, int b) { return (long long)((nra + a - 1) / a) * ((nrb + b - 1) / b); };
@@ -35,6 +49,7 @@ LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
     const int n = t < 256 && units >= (rows ? 32 : 16) ? std::max(1, (int)std::min<long long>(256 / t, units / 4)) : 1;
     q.span = (units + n - 1) / n * 16;
     q.nsplit = (ncb + q.span - 1) / q.span;
+    if (q.tile == LIN_TILE_64 && t * q.nsplit <= 256 && std::min(ncb, q.span) >= 40) q.tile = LIN_TILE_64K;
     q.ldw = (long long)nra * 32;
     return q;
 }

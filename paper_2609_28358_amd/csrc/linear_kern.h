@@ -98,9 +98,9 @@ template <int FA, int FB, class T> struct LinLds {
 };
 
 // tile shapes a launch is asked for: outputs of at most 32 or 64 rows (the
-// contraction is shared by a workgroup's waves), 64 x 64, 128 x 128, 256
-// columns x 128 rows
-enum { LIN_TILE_ROWS32 = 0, LIN_TILE_ROWS64 = 1, LIN_TILE_64 = 2, LIN_TILE_128 = 3, LIN_TILE_256 = 4 };
+// contraction is shared by a workgroup's waves), 64 x 64 without and with a
+// shared contraction, 128 x 128, 256 columns x 128 rows
+enum { LIN_TILE_ROWS32, LIN_TILE_ROWS64, LIN_TILE_64, LIN_TILE_64K, LIN_TILE_128, LIN_TILE_256 };
 
 // linear.hip: workspace bytes and launch of one product (nrows x ncols
 // outputs over ncon, formats and matrices in the order A, B)
@@ -362,13 +362,17 @@ __device__ __forceinline__ v8i lin_frag(const uint8_t* p, int next, int lane) {
     return o;
 }
 
-// Wait until the oldest of `later` + 1 stages of PER copies each is complete.
-template <int PER>
+// Wait until the oldest of `later` + 1 <= MOST + 1 stages of PER copies each is
+// complete.
+template <int PER, int MOST>
 __device__ __forceinline__ void lin_wait(int later) {
-    static_assert(2 * PER <= 63, "two stages in flight must fit the vmcnt counter");
-    if (later <= 0) vm_wait<0>();
-    else if (later == 1) vm_wait<PER>();
-    else vm_wait<2 * PER>();
+    static_assert(MOST * PER <= 63, "the stages in flight must fit the vmcnt counter");
+    if constexpr (MOST == 0) {
+        vm_wait<0>();
+    } else {
+        if (later >= MOST) vm_wait<MOST * PER>();
+        else lin_wait<PER, MOST - 1>(later);
+    }
 }
 
 // ---------------------------------------------------------------- column sums
@@ -451,7 +455,7 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
     constexpr int NA = RA * KB / BA::BPI, NSL = NA + RB * KB / BB::BPI;   // 1 KB copies of a stage
     constexpr int NQ = NSL / W, NSQ = (L::NSI + W - 1) / W, PER = NQ + NSQ;
     static_assert(NSL % W == 0 && RA * KB % BA::BPI == 0 && RB * KB % BB::BPI == 0 && KS % 2 == 0, "whole copies");
-    static_assert(NBUF >= 3 && NBUF <= 5, "ring");
+    static_assert(NBUF >= 3, "ring");
     static_assert(MB * NB <= 16, "accumulators");
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
 
@@ -599,7 +603,7 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
     };
 
     for (int j = 0; j < NBUF - 1 && j < nst; j++) issue(j);
-    lin_wait<PER>(min(NBUF - 2, nst - 1));
+    lin_wait<PER, NBUF - 2>(nst - 1);
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < NB; j++) fetch_b(smem, 0, j, rawb[j], scb[j]);
@@ -613,7 +617,7 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
         constexpr bool AHEAD = decltype(ahead)::value;
         // stage st + 1 is complete for every wave, and stage st - 1's slot is free
         if (AHEAD) vm_wait<(NBUF - 3) * PER>();
-        else if (st + 1 < nst) lin_wait<PER>(min(NBUF - 3, nst - 2 - st));
+        else if (st + 1 < nst) lin_wait<PER, NBUF - 3>(nst - 2 - st);
         __syncthreads();
         const uint8_t* const slot = smem + (buf == 0 ? NBUF - 1 : buf - 1) * L::STAGE;
         if (!AHEAD && st + NBUF - 1 < nst) issue(buf == 0 ? NBUF - 1 : buf - 1);
