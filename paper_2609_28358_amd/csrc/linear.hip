@@ -39,10 +39,12 @@ LinPlan lin_plan(int op, int nra, int nrb, int ncb) {
     q.tb = (nrb + q.rb - 1) / q.rb;
     // a grid that leaves CUs idle is split along a long contraction, in units of
     // 16 blocks (a whole number of any shape's stages), four of them a split at
-    // least.  The join is a launch of its own: 8 rows x 8192 x 1000 take 10.9 us
-    // whole and 15.7 split, 8 x 16384 x 1000 16 either way; 100 x 8192 x 1000 take
-    // 17 split and 18 whole.  (Splitting grids of one round in two did not pay:
-    // 8192 x 4096 x 1024, both gradients, 84 us whole and 96 split.)
+    // least.  The join is a launch of its own, about 4 us of the host.  On the GPU
+    // (forward, MXFP8 / MXFP4, rows x outs x ins): 100 x 1000 x 8192 whole 21.3 /
+    // 12.4, split 11.9 / 9.4 us, x 4096 12.9 / 8.5 and 10.8 / 8.3; 8 x 1000 x 16384
+    // 16.9 / 10.9 and 10.0 / 8.1, x 8192 10.4 / 7.3 and 8.0 / 6.9.  (Splitting
+    // grids of one round in two did not pay: 8192 x 4096 x 1024, both gradients, 84
+    // us whole and 96 split.)
     const long long t = (long long)q.ta * q.tb;
     const int units = (ncb + 15) / 16;
     const bool rows = q.tile == LIN_TILE_ROWS32 || q.tile == LIN_TILE_ROWS64;
@@ -100,7 +102,14 @@ int launch_linear(int op, int fa, int fb, const LinMat& a, const LinMat& b, int 
     p.ldw = q.ldw;
     p.part = q.nsplit > 1 ? (float*)ws : nullptr;
     p.colsum = colsum;
-    p.nsum = colsum ? (nrb + 7) / 8 * 8 : 0;
+    // column sums: up to four workgroups a column block, as many as there is room
+    // for beside the tiles (one of the shared-contraction tiles a CU, two of the
+    // others); where there is none, four short ones delay the tiles least (MXFP8
+    // 8192 x 1024 x 1024 26 us, 39 with one), but past 64 blocks one (16384 x 4096 x
+    // 1024 132 us, 188 with four)
+    const long long room = (q.tile == LIN_TILE_64K ? 256 : 512) - tiles;
+    p.sumsplit = room >= nrb ? (room >= 4 * nrb ? 2 : room >= 2 * nrb ? 1 : 0) : nrb <= 64 ? 2 : 0;
+    p.nsum = colsum ? ((nrb << p.sumsplit) + 7) / 8 * 8 : 0;
     int rc;
     if (fa == MXC_E4M3) rc = launch_linear_e4m3(op, p, q.tile, s);
     else if (fa == MXC_E2M1 && fb == MXC_E2M1) rc = launch_linear_e2m1(op, p, q.tile, s);

@@ -62,7 +62,7 @@ struct LinArgs {
     float* part;          // split contraction: partial sums [split][nrows][ldw], else NULL
     long long ldw;
     float* colsum;        // weight gradient: db, or NULL
-    int nsum;             // workgroups in front of the tiles that form it
+    int nsum, sumsplit;   // workgroups in front of the tiles that form it, log2 of those of a column block
     int ta, tb;           // tiles along A's and B's rows
     int nsplit, span;     // splits of the contraction, blocks of each (whole stages)
 };
@@ -376,62 +376,84 @@ __device__ __forceinline__ void lin_wait(int later) {
 }
 
 // ---------------------------------------------------------------- column sums
-// db: the sums of dZ over its rows, for one of its column blocks -- a product
-// with a row of ones, exact like the others, from fragments that are contiguous
-// in memory.  The waves take pairs of row blocks in turn and are joined in
-// order.  (Taken along by the tiles of the weight gradient, the sums cost every
-// tile 16 or 32 registers: the 256 x 128 tile spilled and ran at a third.)
+// db: the sums of dZ over its rows, for 32, 16 or 8 of its columns (one, two or
+// four workgroups a column block) -- a product with a row of ones, exact like
+// the others, from fragments that are contiguous in memory.  The 32 rows of a
+// fragment are those columns of one, two or four pairs of row blocks; the waves
+// take such groups in turn, LIN_SUM_AHEAD of them in flight, and the parts are
+// joined in order.  (Taken along by the tiles of the weight gradient, the sums
+// cost every tile 16 or 32 registers: the 256 x 128 tile spilled and ran at a
+// third.)
+constexpr int LIN_SUM_AHEAD = 4;
 template <int F, int W>
-__device__ __forceinline__ void lin_colsum(const LinOp& o, float* out, int n, int rb, float* red) {
-    constexpr int SRC = LinBlk<F>::SRC, ROW = SRC / 32;
-    const int lane = threadIdx.x & 63, h = lane >> 5;
+__device__ __forceinline__ void lin_colsum(const LinOp& o, float* out, int n, int part, int split, float* red) {
+    constexpr int SRC = LinBlk<F>::SRC, ROW = SRC / 32, WORDS = ROW / 4;
+    const int cols = 32 >> split, subs = 1 << split;          // columns; pairs of row blocks in a fragment
+    const int rb = part >> split, first = (part & (subs - 1)) * cols;
+    const int lane = threadIdx.x & 63, h = lane >> 5, col = first + (lane & (cols - 1)), sub = (lane & 31) >> (5 - split);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (rb >= o.nrb) return;
     v16f acc;
 #pragma unroll
     for (int e = 0; e < 16; e++) acc[e] = 0.0f;
     const int pairs = (o.ncb + 1) / 2;
-#pragma unroll 4
-    for (int p = wave; p < pairs; p += W) {
-        const int k0 = 2 * p, k1 = min(2 * p + 1, o.ncb - 1);
-        const bool two = 2 * p + 1 < o.ncb;
-        const size_t b0 = (size_t)rb * o.srow + (size_t)k0 * o.scon, b1 = (size_t)rb * o.srow + (size_t)k1 * o.scon;
-        const int s0 = o.scales[b0], s1 = two ? o.scales[b1] : 0;
-        v8i f;
-        if constexpr (F == MXC_E4M3) {
-            const int at = (lane & 31) * ROW + 16 * h;
-            const v4i u = *(const v4i*)(o.codes + b0 * SRC + at), w = *(const v4i*)(o.codes + b1 * SRC + at);
+    for (int g = wave; g * subs < pairs; g += W * LIN_SUM_AHEAD) {
+        uint32_t f[LIN_SUM_AHEAD][8];
+        int s0[LIN_SUM_AHEAD], s1[LIN_SUM_AHEAD];
 #pragma unroll
-            for (int e = 0; e < 4; e++) { f[e] = u[e]; f[4 + e] = two ? w[e] : 0; }
-            uint32_t one[16], d[16];
+        for (int k = 0; k < LIN_SUM_AHEAD; k++) {
+            // blocks past the end: the last one is read and counts as zeros
+            const int c0 = 2 * (subs * (g + k * W) + sub), c1 = c0 + 1;
+            const size_t b0 = (size_t)rb * o.srow + (size_t)min(c0, o.ncb - 1) * o.scon;
+            const size_t b1 = (size_t)rb * o.srow + (size_t)min(c1, o.ncb - 1) * o.scon;
+            s0[k] = o.scales[b0];
+            s1[k] = o.scales[b1];
+            if constexpr (F == MXC_E4M3) {
+                const v4i u = *(const v4i*)(o.codes + b0 * SRC + col * ROW + 16 * h);
+                const v4i w = *(const v4i*)(o.codes + b1 * SRC + col * ROW + 16 * h);
 #pragma unroll
-            for (int e = 0; e < 16; e++) one[e] = 0x3F803F80u;
-            e4m3_decode32(f, s0, s1, d);
-            acc = mfma_x8(one, d, acc);
-        } else {
-            const uint8_t* q = o.codes + (h ? b1 : b0) * SRC + (lane & 31) * ROW;
-            const bool ok = two || !h;
+                for (int e = 0; e < 4; e++) { f[k][e] = c0 < o.ncb ? u[e] : 0; f[k][4 + e] = c1 < o.ncb ? w[e] : 0; }
+            } else {
+                const uint8_t* q = o.codes + (h ? b1 : b0) * SRC + col * ROW;
+                const bool ok = (h ? c1 : c0) < o.ncb;
 #pragma unroll
-            for (int e = 0; e < 8; e++) f[e] = 0;
+                for (int e = 0; e < 8; e++) f[k][e] = 0;
 #pragma unroll
-            for (int e = 0; e < ROW / 8; e++) {
-                const v2i u = *(const v2i*)(q + 8 * e);
-                f[2 * e] = ok ? u[0] : 0;
-                f[2 * e + 1] = ok ? u[1] : 0;
+                for (int e = 0; e < WORDS; e += 2) {
+                    const v2i u = *(const v2i*)(q + 4 * e);
+                    f[k][e] = ok ? u[0] : 0;
+                    f[k][e + 1] = ok ? u[1] : 0;
+                }
             }
-            v8i one;                              // E2M1 code 2 is 1.0
+            s0[k] = c0 < o.ncb ? s0[k] : 0;
+            s1[k] = c1 < o.ncb ? s1[k] : 0;
+        }
 #pragma unroll
-            for (int e = 0; e < 8; e++) one[e] = e < 4 ? 0x22222222 : 0;
-            acc = mfma_mx<MXC_E2M1, F>(one, f, acc, 127, h ? s1 : s0);
+        for (int k = 0; k < LIN_SUM_AHEAD; k++) {
+            v8i v;
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = f[k][e];
+            if constexpr (F == MXC_E4M3) {
+                uint32_t one[16], d[16];
+#pragma unroll
+                for (int e = 0; e < 16; e++) one[e] = 0x3F803F80u;
+                e4m3_decode32(v, s0[k], s1[k], d);
+                acc = mfma_x8(one, d, acc);
+            } else {
+                v8i one;                          // E2M1 code 2 is 1.0
+#pragma unroll
+                for (int e = 0; e < 8; e++) one[e] = e < 4 ? 0x22222222 : 0;
+                acc = mfma_mx<MXC_E2M1, F>(one, v, acc, 127, h ? s1[k] : s0[k]);
+            }
         }
     }
     if (lane < 32) red[wave * 32 + lane] = acc[0];
     __syncthreads();
-    if (threadIdx.x < 32 && rb * 32 + (int)threadIdx.x < n) {
-        float v = red[threadIdx.x];
-#pragma unroll
-        for (int w = 1; w < W; w++) v += red[w * 32 + threadIdx.x];
-        out[rb * 32 + threadIdx.x] = v;
+    const int c = rb * 32 + first + (int)threadIdx.x;
+    if ((int)threadIdx.x < cols && c < n) {
+        float v = 0.0f;
+        for (int w = 0; w < W * subs; w++) v += red[w * cols + threadIdx.x];
+        out[c] = v;
     }
 }
 
@@ -468,7 +490,7 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
     int bid = blockIdx.x;
     if constexpr (OP == LIN_WGRAD) {
         if (bid < p.nsum) {
-            lin_colsum<FB, W>(p.b, p.colsum, p.e.nrows, bid, (float*)smem);
+            lin_colsum<FB, W>(p.b, p.colsum, p.e.nrows, bid, p.sumsplit, (float*)smem);
             return;
         }
         bid -= p.nsum;
@@ -748,6 +770,8 @@ __global__ __launch_bounds__(T::W * 64, 2) void linear_kernel(const LinArgs p) {
 
 template <int FA, int FB, int OP, class T>
 int linear_launch(const LinArgs& a, hipStream_t s) {
+    // the plan counted tiles of this shape: one that begins past the last block would read out of range
+    if (a.ta != (a.a.nrb + T::RA - 1) / T::RA || a.tb != (a.b.nrb + T::RB - 1) / T::RB || a.span % T::KB) return MXC_ERR_SHAPE;
     static std::atomic<uint64_t> devs{0};
     constexpr int lds = LinLds<FA, FB, T>::BYTES;
     static_assert(lds <= 163840, "LDS of a CU");
