@@ -342,3 +342,65 @@ def test_pointers_at_any_element(mx, dtype, size):
         for name, ref, (buf, v) in zip(("y", "pre", "dx", "dw", "db"), (y, pre, dx, dw, db), bufs):
             assert torch.equal(v, ref), name
             assert (buf[:k] == 9).all() and (buf[k + ref.numel():] == 9).all(), name
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1", "e2m3"])
+@pytest.mark.parametrize("size", [(333, 700, 2500), (333, 700, 1000), (1300, 600, 1900), (1, 32, 33), (95, 5000, 2112),
+                                  (4129, 40, 70), (8200, 40, 33)], ids=lambda s: "x".join(map(str, s)))
+def test_column_sums(mx, fmt, size):
+    """db by one, two and four workgroups a column block, an odd number of row
+    blocks, rows that end inside a block; dw does not depend on it.  Bound as in
+    test_backward."""
+    rows, ins, outs = size
+    f = mm.FORMATS[fmt][0]
+    x, _ = mm.matrix(mx, rows, ins, f, 500)
+    dz, gv = mm.matrix(mx, rows, outs, f, 501, std=1e-3)
+    dw, db = mx.linear_wgrad(dz, x)
+    mm.check(db, gv.sum(0), (rows / 16 + 32) * 2.0 ** -23 * np.abs(gv).sum(0), torch.float32, "db")
+    assert torch.equal(dw, mx.linear_wgrad(dz, x, bias=False)[0])
+    for _ in range(3):
+        assert torch.equal(db, mx.linear_wgrad(dz, x)[1])
+
+
+@pytest.mark.parametrize("fmt", list(mm.FORMATS))
+def test_long_contractions_of_small_grids(mx, fmt):
+    """One 64 x 64 tile a CU at most, from 40 blocks of the contraction on, in
+    every product; ragged in all three sizes, with everything the epilogue takes."""
+    fw, fx = mm.FORMATS[fmt]
+    for rows, ins, outs in ((100, 1281, 130), (70, 1250, 333), (129, 3001, 65)):
+        x, xv = mm.matrix(mx, rows, ins, fx, 510)
+        w, wv = mm.matrix(mx, outs, ins, fw, 511, std=ins ** -0.5)
+        bias, res = _rand((outs,), 512, torch.float32), _rand((rows, outs), 513, torch.bfloat16)
+        pre = torch.empty_like(res)
+        y = mx.linear(w, x, bias=bias, fn=2, residual=res, dtype=torch.bfloat16, pre_out=pre)
+        z, tz, yr, ty = _fwd_ref(xv, wv, bias, 2, res)
+        mm.check(pre, z, tz, torch.bfloat16, "pre")
+        mm.check(y, yr, ty, torch.bfloat16, "y")
+        # the same sizes with the roles of the products exchanged
+        x, xv = mm.matrix(mx, ins, rows, fx, 514)
+        dz, gv = mm.matrix(mx, ins, outs, fw, 515, std=1e-3)
+        dw, db = mx.linear_wgrad(dz, x)
+        mm.check(dw, gv.T @ xv, mm.product_tol(gv.T, xv.T), torch.float32, "dw")
+        mm.check(db, gv.sum(0), (ins / 16 + 32) * 2.0 ** -23 * np.abs(gv).sum(0), torch.float32, "db")
+        dz, gv = mm.matrix(mx, rows, ins, fw, 516, std=1e-3)
+        w, wv = mm.matrix(mx, ins, outs, fw, 517)
+        add = _rand((rows, outs), 518, torch.float32, 1e-3)
+        dx = mx.linear_dgrad(w, dz, add=add, dtype=torch.float32)
+        ref = gv @ wv + _np(add)
+        mm.check(dx, ref, mm.product_tol(gv, wv.T) + mm.U * np.abs(ref), torch.float32, "dx")
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "e2m1", "e2m3"])
+@pytest.mark.parametrize("rows", [70, 97, 321])
+def test_nonfinite_column_sums(mx, fmt, rows):
+    """A NaN in the last row makes the sums of its block's 32 columns NaN and no
+    others: row blocks that do not exist count as zeros."""
+    f = mm.FORMATS[fmt][0]
+    g = _rand((rows, 100), 1, torch.float32)
+    x, _ = mm.matrix(mx, rows, 40, f, 2)
+    base = mx.linear_wgrad(mx.quantize_matrix(g, f), x)[1]
+    g[rows - 1, 70] = float("nan")
+    db = mx.linear_wgrad(mx.quantize_matrix(g, f), x)[1]
+    bad = torch.zeros(100, dtype=torch.bool, device=DEV)
+    bad[64:96] = True
+    assert torch.equal(torch.isnan(db), bad) and torch.equal(db[~bad], base[~bad])
