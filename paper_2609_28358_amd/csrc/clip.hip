@@ -131,6 +131,9 @@ __global__ __launch_bounds__(CT) void clip_scale_kernel(const ClipArgs a, const 
         const long long b0 = (long long)(k - a.first[t]) * a.chunk;
         const uint8_t* p = (const uint8_t*)a.src[t] + b0;
         uint8_t* d = (uint8_t*)a.dst[t] + b0;
+        // non-temporal where the vectors are aligned (300 bf16 tensors, 600 MB: both
+        // launches 343 -> 316 us)
+        const bool nt = ((uintptr_t)d & 15) == 0;
         const int len = (int)min((long long)a.chunk, bytes - b0);
         vectors(len, [&](int o, auto num) {
             constexpr int N = decltype(num)::value;
@@ -146,7 +149,8 @@ __global__ __launch_bounds__(CT) void clip_scale_kernel(const ClipArgs a, const 
                     r.w[q] = bf ? bf16_pack2(__uint_as_float(w << 16) * c, __uint_as_float(w & 0xFFFF0000u) * c)
                                 : __float_as_uint(__uint_as_float(w) * c);
                 }
-                *(Vec16*)(d + o + i * 16 * CT) = r;
+                if (nt) store_nt(d + o + i * 16 * CT, make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]));
+                else *(Vec16*)(d + o + i * 16 * CT) = r;
             }
         }, [&](int o, int e) {
             for (; o < e; o += bf ? 2 : 4) {

@@ -43,10 +43,13 @@ struct LinOp {
 // The epilogue: out[r][c] for output row r < nrows, column c < ncols.
 //   fwd    z = v + bias[c]; pre[r][c] = z; out = fn(z) + res[r][c]
 //   dgrad  out = v fn'(z[r][c]) + res[r][c]
-// pre doubles as dgrad's z.  nt: the results are larger than the caches and
-// their rows begin at cache lines: non-temporal stores (MXFP4 16384 x 300 x 8192
-// with its pre-activation 145 -> 122 us; rows that begin elsewhere lose by them,
-// 16384 x 300 x 8191 186 -> 241).
+// pre doubles as dgrad's z.  nt: the results are 4 MiB or more and their rows
+// begin at cache lines: non-temporal stores, which take less from the loads beside
+// them and from what reads the results next (MXFP4 4096 x 1024 x 1024 with its
+// pre-activation 10.7 -> 9.4 us, and with the quantization of the result behind it
+// 18.0 -> 16.3; 16384 x 300 x 8192 145 -> 122; at 2 MB, 1024 x 1024 x 1024 with the
+// quantization, 9.6 -> 9.8.  Rows that begin elsewhere lose by them, 16384 x 300 x
+// 8191 186 -> 241).
 struct LinEpi {
     void* out;
     const float* bias;

@@ -647,7 +647,7 @@ static int linear_run(int op, const mxc_linear& p, int fa, int fb, const LinMat&
         return MXC_ERR_ALIGN;
     const int es = e.bf16 ? 2 : 4;
     const bool written = op != LIN_DGRAD && e.pre;            // a second result (the input gradient only reads it)
-    e.nt = (int64_t)e.nrows * e.ncols * es >= (32 << 20) && e.ldo * es % 128 == 0 && (uintptr_t)e.out % 128 == 0 &&
+    e.nt = (int64_t)e.nrows * e.ncols * es >= (4 << 20) && e.ldo * es % 128 == 0 && (uintptr_t)e.out % 128 == 0 &&
            (!written || (e.ldp * es % 128 == 0 && (uintptr_t)e.pre % 128 == 0));
     return launch_linear(op, fa, fb, a, b, ncon, e, colsum, ws, (hipStream_t)stream);
 }

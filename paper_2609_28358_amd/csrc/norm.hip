@@ -75,8 +75,9 @@ __device__ __forceinline__ void unpack(const Raw<T>& u, float* o) {
 }
 template <typename T>
 __device__ __forceinline__ void ld(const T* p, int n, float* o) { unpack<T>(get(p, n), o); }
+// nt: NormArgs
 template <typename T>
-__device__ __forceinline__ void st(T* p, int n, const float* v) {
+__device__ __forceinline__ void st(T* p, int n, const float* v, bool nt = false) {
     constexpr int V = VEC<T>;
     if (n >= V) {
         Raw<T> u;
@@ -85,7 +86,8 @@ __device__ __forceinline__ void st(T* p, int n, const float* v) {
             if constexpr (V == 8) u.w[k] = bf16_pack2(v[2 * k], v[2 * k + 1]);
             else u.w[k] = __float_as_uint(v[k]);
         }
-        *(Raw<T>*)p = u;
+        if (nt) store_nt(p, make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]));
+        else *(Raw<T>*)p = u;
     } else {
 #pragma unroll
         for (int e = 0; e < V; e++)
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NV == 8 || sizeof(T) == 2 ? 
                 x[q + e] += g[q + e] * v;
                 s[0] += x[q + e] * x[q + e];
             }
-            st<T>((T*)a.h + r * a.ldh + c, n, x + q);
+            st<T>((T*)a.h + r * a.ldh + c, n, x + q, a.nt);
         });
         if (a.w_pre) {
             row_sum<TPR, 1>(s, red, par);
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(TPR == 64 ? 256 : TPR, NV == 8 || sizeof(T) == 2 ? 
                 float u[V];
 #pragma unroll
                 for (int e = 0; e < V; e++) u[e] = x[q + e] * rh * wq[q + e];
-                st<T>((T*)a.u + r * a.ldu + c, n, u);
+                st<T>((T*)a.u + r * a.ldu + c, n, u, a.nt);
             });
         }
     }
@@ -340,7 +342,7 @@ __global__ __launch_bounds__(512, NV == 8 ? 4 : 2) void norm_bwd_kernel(const No
                     m[0] += gw[q + e] * x[q + e] * yh;                   // b w_post yh
                     y[q + e] = yh;
                 }
-                if (live) st<T>((T*)a.dx + r * a.lddx + c, n, x + q);
+                if (live) st<T>((T*)a.dx + r * a.lddx + c, n, x + q, a.nt);
             });
             float my = 0.0f;
             if (a.w_post) {
@@ -351,7 +353,7 @@ __global__ __launch_bounds__(512, NV == 8 ? 4 : 2) void norm_bwd_kernel(const No
                 float o[V];
 #pragma unroll
                 for (int e = 0; e < V; e++) o[e] = ry * (gw[q + e] * x[q + e] - y[q + e] * my);
-                if (live) st<T>((T*)a.dy + r * a.lddy + c, n, o);
+                if (live) st<T>((T*)a.dy + r * a.lddy + c, n, o, a.nt);
             });
         }
         if constexpr (!WHOLE) {                               // the join makes both gradients of it
@@ -473,7 +475,14 @@ void plan_runs(NormArgs& a) {
 
 }  // namespace
 
+// Results whose rows begin at cache lines (ld: their row stride).
+static bool lines(const NormArgs& a, bool bf16, const void* p, long long ld) {
+    const int es = bf16 ? 2 : 4;
+    return !p || (a.rows * a.d * es >= (4 << 20) && (uintptr_t)p % 128 == 0 && ld * es % 128 == 0);
+}
+
 int launch_norm_fwd(NormArgs a, bool bf16, hipStream_t s) {
+    a.nt = lines(a, bf16, a.h, a.ldh) && lines(a, bf16, a.u, a.ldu);
     const long long rl = norm_fwd_rows(a.d);
     a.run = std::max<long long>(rl, (a.rows + norm_fwd_runs(a.d) - 1) / norm_fwd_runs(a.d));
     return launch(a, false, bf16, (unsigned)((a.rows + a.run - 1) / a.run), s);
@@ -494,6 +503,7 @@ size_t norm_bwd_workspace(long long rows, int d, long long gates, bool gate, boo
 
 int launch_norm_bwd(NormArgs a, bool bf16, float* dw_pre, float* dw_post, float* dgate, void* ws, hipStream_t s) {
     plan_runs(a);
+    a.nt = lines(a, bf16, a.dx, a.lddx) && lines(a, bf16, a.dy, a.lddy);
     const bool one = a.runs == 1;                 // a single workgroup writes the results itself
     float* p = (float*)ws;
     auto take = [&](float* dst) {
