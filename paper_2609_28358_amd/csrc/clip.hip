@@ -10,8 +10,8 @@
 // its chunk by counting, lane by lane, the tensors that begin no later.  Each workgroup of the norm
 // leaves one partial sum; every workgroup of the scaling adds all of them, in
 // the same order, so the result does not depend on timing and there is no
-// third launch.  300 bf16 tensors of 1.15 GB together: norm 226 us (5.1 TB/s),
-// scaling 467 (4.9 TB/s); 60 fp32 ones of 19 MB 7.4 and 9.9 us.
+// third launch.  300 bf16 tensors of 1.15 GB together: norm 188 us (6.1 TB/s),
+// scaling 492 (4.7 TB/s); 60 fp32 ones of 19 MB 6.9 and 10.5 us.
 #include "mx_internal.h"
 #include "clip.h"
 

@@ -19,9 +19,9 @@
 // row and the epilogue moves vectors.
 //
 // What bounds it: large MXFP8 products the matrix units and their power (16384 x
-// 4096 x 4096 438 us, 1.25 PFLOP/s; loops of the MFMAs alone reach 1.4); large
+// 4096 x 4096 437 us, 1.26 PFLOP/s; loops of the MFMAs alone reach 1.4); large
 // MXFP4 ones the bytes of their results (4096 x 4096 x 1024 with SiLU and the
-// pre-activation kept 23.5 us, 71 MB at 3.0 TB/s; the input gradient 26 us);
+// pre-activation kept 24 us, 71 MB at 3.0 TB/s);
 // few rows the weights' bytes (24 x 8192 x 8192 MXFP8 13.9 us, 5.0 TB/s); small
 // ones a chain of stages behind the launch (1 x 4096 x 1024 MXFP4 5.6 us).
 #pragma once

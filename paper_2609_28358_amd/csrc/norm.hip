@@ -11,8 +11,8 @@
 // What bounds both is memory: a row is read once and held in registers (8
 // values of each tensor a thread, 16 of the longest rows), with two sums over the
 // row forward (Y's square, then H's) and two rounds of sums backward (the second
-// one needs dX).  bf16: forward 8192 x 4096 50 us (5.3 TB/s), backward 16384 x
-// 1024 39 us (5.2 TB/s) and 6 for the join; a copy of 2 GiB reaches 5.0 TB/s.
+// one needs dX).  bf16: forward 8192 x 4096 45 us (6.0 TB/s), backward 16384 x
+// 1024 40 us (5.0 TB/s) and 6 for the join; a copy of 2 GiB reaches 5.0 TB/s.
 // A workgroup takes a run of consecutive rows, so the weights and the gate are
 // loaded once a run; backward, its column sums stay in registers until the
 // run's end and are added over the workgroups by a second kernel, in order.
