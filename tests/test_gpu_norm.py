@@ -282,3 +282,29 @@ def test_pointers_at_any_element(mx, dtype, d):
         mx.norm_residual_backward(put(dh, k), put(du, k + 1), put(h, k + 2), put(y, k), dx_out=o[0], dy_out=o[1],
                                   dw_pre_out=o[2], dw_post_out=o[3], dgate_out=o[4], **p)
         same(grads, bufs, k)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows,d", [(1100, 2048), (1100, 2112), (4200, 520)])
+def test_results_of_several_mebibytes(mx, dtype, rows, d):
+    """Results in whole cache lines (and rows of 520, which are none in bf16):
+    the bits of the same results at one element past a line, and of strided
+    ones, whose padding stays."""
+    case = (rows, d, 2, True, True)
+    x, y, wp, wq, g = _case(case, dtype, 950)
+    dh, du = _rand((rows, d), 960, dtype), _rand((rows, d), 961, dtype)
+    kw = dict(w_post=wp, gate=g, w_pre=wq, scale=0.7, eps=EPS)
+    h, u = mx.norm_residual(x, y, **kw)
+    dx, dy = mx.norm_residual_backward(dh, du, h, y, **kw)[:2]
+    off = [torch.empty(rows * d + 1, dtype=dtype, device=DEV)[1:].view(rows, d) for _ in range(4)]
+    wide = [torch.full((rows, d + 128), 9.0, dtype=dtype, device=DEV) for _ in range(4)]
+    for o in (off, [w[:, :d] for w in wide]):
+        mx.norm_residual(x, y, h_out=o[0], u_out=o[1], **kw)
+        mx.norm_residual_backward(dh, du, h, y, dx_out=o[2], dy_out=o[3], **kw)
+        for a, b in zip((h, u, dx, dy), o):
+            assert torch.equal(a, b)
+    for w in wide:
+        assert (w[:, d:] == 9).all()
+    ref = _bwd_ref(*(_np(t[:8]) for t in (dh, du, h, y)), _np(wp), _np(wq), _np(g[:1]), float(np.float32(0.7)))
+    mm.check(dx[:8], *ref["dx"], dtype, "dx")
+    mm.check(dy[:8], *ref["dy"], dtype, "dy")
