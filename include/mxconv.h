@@ -686,7 +686,9 @@ int mxconv_quantize_sum_sr(int fmt, int n, int c, int h, int w, int nterms, cons
  *   workspace  device, >= mxconv_linear_workspace_bytes(op, lin) bytes (may be
  *              NULL when that is 0): partial sums of a product whose
  *              contraction is split over workgroups, added in a fixed order.
- * fn: MXC_FN_NONE, MXC_FN_RELU or MXC_FN_SILU without flags.
+ * fn: MXC_FN_NONE, MXC_FN_RELU or MXC_FN_SILU without flags.  Here MXC_FN_RELU
+ * keeps a NaN (the convolutions' makes it 0), and its gradient is 0 where z <= 0,
+ * whatever the product, and the product elsewhere.
  * Errors: NULL, ARG (enum, sizes, strides), SHAPE (a matrix too large),
  * ALIGN, WORKSPACE, HIP. */
 #define MXC_LINEAR_MAX_DIM (1 << 20)

@@ -137,14 +137,16 @@ __device__ __forceinline__ void dma16_base(const uint8_t* base, uint32_t off, ui
 
 // ---------------------------------------------------------------- epilogue
 // No contraction: every path (vectors, columns, joined splits) gives the same bits.
+// ReLU keeps a NaN, and its gradient chooses instead of multiplying by 0 or 1: zero
+// where z <= 0, whatever the product, and the product elsewhere.
 template <int OP>
 __device__ __forceinline__ float lin_value(int fn, float v, float b, float z, float r) {
 #pragma clang fp contract(off)
     if constexpr (OP == LIN_FWD) {
         v += b;
-        return (fn == MXC_FN_NONE ? v : fn == MXC_FN_RELU ? fn_apply_c<MXC_FN_RELU>(v) : fn_apply_c<MXC_FN_SILU>(v)) + r;
+        return (fn == MXC_FN_NONE ? v : fn == MXC_FN_RELU ? (v <= 0.0f ? 0.0f : v) : fn_apply_c<MXC_FN_SILU>(v)) + r;
     } else if constexpr (OP == LIN_DGRAD) {
-        return (fn == MXC_FN_NONE ? v : v * fn_grad(fn, z)) + r;
+        return (fn == MXC_FN_NONE ? v : fn == MXC_FN_RELU ? (z <= 0.0f ? 0.0f : v) : v * fn_grad_c<MXC_FN_SILU>(z)) + r;
     } else {
         return v;
     }
