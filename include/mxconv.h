@@ -773,14 +773,16 @@ int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void
  * of n >= 0 elements, fp32 or bf16 each, and need no more than their elements'
  * alignment (slices of one buffer).
  *   dst        every tensor's output (its src: in place), or NULL in all of
- *              them: only the norm is formed.  Outputs must not overlap each
- *              other, or a src other than their own.
+ *              them: only the norm is formed.  What is written (outputs, norm,
+ *              workspace) must not overlap, nor a src, but for outputs that are
+ *              their own src: an ARG error.
  *   max_norm   >= 0 (infinity: a finite norm is never scaled).
  *   norm       NULL, or device fp32 [1], written (0 for no elements).
  *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes, 16-byte aligned.
  * The factor is read on the device: no synchronization.  count >= 0; a launch
  * takes 448 tensors, more take several.
- * Errors: NULL, ARG, SHAPE (more than 2^40 elements), ALIGN, WORKSPACE, HIP. */
+ * Errors: NULL, ARG, SHAPE (more than 2^40 elements), ALIGN, WORKSPACE (also: no
+ * host memory to compare the tensors' ranges), HIP. */
 typedef struct mxc_gtensor {
     const void* src;
     void* dst;

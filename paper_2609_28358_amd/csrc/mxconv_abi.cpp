@@ -1,8 +1,11 @@
 // mxconv_abi.cpp -- the C ABI of include/mxconv.h: host-side validation,
 // size helpers and dispatch to the gfx950 kernels.  Every argument check runs
 // on the host before anything is enqueued.
+#include <algorithm>
 #include <cmath>
+#include <memory>
 #include <mutex>
+#include <new>
 
 #include "clip.h"
 #include "linear_kern.h"
@@ -774,6 +777,41 @@ int mxconv_norm_bwd(const mxc_norm* p, const void* dh, int64_t lddh, const void*
 // ---- gradient clipping
 size_t mxconv_grad_clip_workspace_bytes(void) { return (size_t)CLIP_PARTS * sizeof(double); }
 
+// Whether something that is written -- an output, the norm, the workspace --
+// shares bytes with another written range, or with a source that is not that
+// output itself.  The written ranges are put in order; then a neighbour that
+// begins before the end is an overlap, and a source is looked up by its last
+// byte.  (Addresses that wrap around are not met: they are real allocations'.)
+static int clip_disjoint(int count, const mxc_gtensor* t, const float* norm, const void* ws, size_t ws_bytes) {
+    struct Span {
+        uintptr_t begin, end;
+    };
+    Span few[258];
+    std::unique_ptr<Span[]> many;
+    Span* w = few;
+    if (count > 256) {
+        many.reset(new (std::nothrow) Span[count + 2]);
+        if (!(w = many.get())) return MXC_ERR_WORKSPACE;
+    }
+    auto span = [](const void* p, uint64_t bytes) { return Span{(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}; };
+    auto bytes = [](const mxc_gtensor& g) { return (uint64_t)g.n * (g.dtype == MXC_BF16 ? 2 : 4); };
+    int n = 0;
+    for (int i = 0; i < count; i++)
+        if (t[i].n && t[i].dst) w[n++] = span(t[i].dst, bytes(t[i]));
+    if (norm) w[n++] = span(norm, sizeof(float));
+    w[n++] = span(ws, ws_bytes);
+    std::sort(w, w + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+    for (int i = 1; i < n; i++)
+        if (w[i].begin < w[i - 1].end) return MXC_ERR_ARG;
+    for (int i = 0; i < count; i++) {
+        if (!t[i].n || t[i].src == t[i].dst) continue;        // in place: in the order already
+        const Span s = span(t[i].src, bytes(t[i]));
+        const Span* e = std::lower_bound(w, w + n, s.end, [](const Span& a, uintptr_t v) { return a.begin < v; });
+        if (e != w && e[-1].end > s.begin) return MXC_ERR_ARG;
+    }
+    return MXC_OK;
+}
+
 int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* norm, void* workspace, size_t ws_bytes,
                      void* stream) {
     if (count < 0 || count > MXC_CLIP_MAX || !(max_norm >= 0.0)) return MXC_ERR_ARG;
@@ -793,6 +831,7 @@ int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* no
     }
     const bool scale = full >= 0 && t[full].dst;
     if (!scale && !norm) return full >= 0 ? MXC_ERR_NULL : MXC_OK;   // nothing to write
+    if (const int rc = clip_disjoint(count, t, norm, workspace, mxconv_grad_clip_workspace_bytes())) return rc;
     return launch_grad_clip(count, t, scale, max_norm, norm, workspace, (hipStream_t)stream);
 }
 

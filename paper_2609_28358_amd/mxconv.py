@@ -914,8 +914,6 @@ def _clip(tensors, outs, max_norm, norm_out, workspace, stream):
             if osizes != sizes or otypes != types:
                 raise MxconvError("an output must have its gradient's size and type")
         desc[1::4] = array("q", dst)
-        if len(set(dst)) != len(dst) and len(set(full := [p for p, n in zip(dst, sizes) if n])) != len(full):
-            raise MxconvError("a tensor is written twice")
     return _launch(_clip_launch, dev, stream, len(ptrs), desc, max_norm, norm_out, workspace, dev)
 
 
@@ -942,7 +940,8 @@ def grad_norm(tensors, norm_out=None, workspace=None, stream=None):
 def grad_clip(tensors, max_norm, out=None, norm_out=None, workspace=None, stream=None):
     """Scale the tensors (contiguous fp32 or bf16) by min(1, max_norm / (norm +
     1e-6)), norm = their Euclidean norm together, into `out` (tensors of the
-    same sizes and types; None: in place).  Returns the norm before scaling, an
+    same sizes and types, sharing no memory with each other or with a gradient
+    other than their own; None: in place).  Returns the norm before scaling, an
     fp32 device scalar; nothing is synchronized (mxconv_grad_clip)."""
     tensors = list(tensors)
     return _clip(tensors, tensors if out is None else out, max_norm, norm_out, workspace, stream)
