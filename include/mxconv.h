@@ -781,7 +781,7 @@ int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void
  *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes, 16-byte aligned.
  * The factor is read on the device: no synchronization.  count >= 0; a launch
  * takes 448 tensors, more take several.
- * Errors: NULL, ARG, SHAPE (more than 2^40 elements), ALIGN, WORKSPACE (also: no
+ * Errors: NULL, ARG, SHAPE (more than 2^40 elements together), ALIGN, WORKSPACE (also: no
  * host memory to compare the tensors' ranges), HIP. */
 typedef struct mxc_gtensor {
     const void* src;

@@ -821,13 +821,14 @@ int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* no
     int full = -1;                                            // a tensor that is not empty
     int64_t total = 0;
     for (int i = 0; i < count; i++) {
-        if (t[i].n < 0 || t[i].n > (1ll << 36) || (t[i].dtype != MXC_F32 && t[i].dtype != MXC_BF16)) return MXC_ERR_ARG;
+        if (t[i].n < 0 || (t[i].dtype != MXC_F32 && t[i].dtype != MXC_BF16)) return MXC_ERR_ARG;
         if (!t[i].n) continue;                                // an empty tensor's pointers are not looked at
         if (full < 0) full = i;
         if (!t[i].src) return MXC_ERR_NULL;
         if (!t[i].dst != !t[full].dst) return MXC_ERR_ARG;    // outputs for all tensors or for none
         if (!aligned_to(t[i].dtype, t[i].src) || !aligned_to(t[i].dtype, t[i].dst)) return MXC_ERR_ALIGN;
-        if ((total += t[i].n) > (1ll << 40)) return MXC_ERR_SHAPE;
+        if (t[i].n > (1ll << 40) - total) return MXC_ERR_SHAPE;   // by the chunks of 64 KiB that 32 bits count
+        total += t[i].n;
     }
     const bool scale = full >= 0 && t[full].dst;
     if (!scale && !norm) return full >= 0 ? MXC_ERR_NULL : MXC_OK;   // nothing to write
