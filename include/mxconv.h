@@ -668,7 +668,8 @@ int mxconv_quantize_sum_sr(int fmt, int n, int c, int h, int w, int nterms, cons
  * more than their elements' alignment; codes, scales and the workspace are
  * 16-byte aligned.
  * rows at most MXC_LINEAR_MAX_ROWS, outs and ins at most MXC_LINEAR_MAX_DIM, each
- * at least 1.
+ * at least 1; the result of Y or dX at most 2^23 tiles of 128 rows x 256 columns
+ * (all rows with 256 columns), of dW 2^22.
  *
  * Forward:  Y = fn(Z) + residual.
  *   bias      NULL, or device fp32 [outs].

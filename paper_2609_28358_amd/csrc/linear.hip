@@ -79,6 +79,11 @@ int lin_blocks(int n) { return (n + 31) / 32; }
 
 }  // namespace
 
+bool linear_fits(int op, int nrows, int ncols) {
+    const long long tiles = (long long)((lin_blocks(ncols) + 7) / 8) * ((lin_blocks(nrows) + 3) / 4);
+    return tiles <= (op == LIN_WGRAD ? 1 << 22 : 1 << 23);
+}
+
 size_t linear_workspace(int op, int nrows, int ncols, int ncon) {
     const LinPlan q = lin_plan(op, lin_blocks(ncols), lin_blocks(nrows), lin_blocks(ncon));
     if (q.nsplit == 1) return 0;
@@ -90,7 +95,6 @@ int launch_linear(int op, int fa, int fb, const LinMat& a, const LinMat& b, int 
     const int nra = lin_blocks(e.ncols), nrb = lin_blocks(e.nrows), ncb = lin_blocks(ncon);
     const LinPlan q = lin_plan(op, nra, nrb, ncb);
     const long long tiles = (long long)q.ta * q.tb * q.nsplit;
-    if (tiles > (1 << 22)) return MXC_ERR_SHAPE;
     LinArgs p;
     // blocks are stored [row block][column block] of the matrix: along the
     // product's rows where those are the matrix's rows, else along its columns

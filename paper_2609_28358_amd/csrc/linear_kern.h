@@ -112,8 +112,11 @@ template <int FA, int FB, class T> struct LinLds {
 // shared contraction, 128 x 128, 256 columns x 128 rows
 enum { LIN_TILE_ROWS32, LIN_TILE_ROWS64, LIN_TILE_64, LIN_TILE_64K, LIN_TILE_128, LIN_TILE_256 };
 
-// linear.hip: workspace bytes and launch of one product (nrows x ncols
-// outputs over ncon, formats and matrices in the order A, B)
+// linear.hip: whether a product's tiles fit a launch (half of a grid's 2^32
+// threads: workgroups of 256, up to 512 for the weight gradient), its workspace
+// bytes and its launch (nrows x ncols outputs over ncon, formats and matrices in
+// the order A, B)
+bool linear_fits(int op, int nrows, int ncols);
 size_t linear_workspace(int op, int nrows, int ncols, int ncon);
 int launch_linear(int op, int fa, int fb, const LinMat& a, const LinMat& b, int ncon, const LinEpi& e, float* colsum,
                   void* ws, hipStream_t s);

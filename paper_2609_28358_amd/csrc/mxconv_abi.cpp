@@ -617,21 +617,24 @@ static int linear_fmts(int fmt, int* f1, int* f2) {
     return fmt_ok(*f1) && fmt_ok(*f2) && pair_ok(*f1, *f2) ? MXC_OK : MXC_ERR_ARG;
 }
 
-static int linear_check(const mxc_linear* p) {
-    if (p->rows <= 0 || p->outs <= 0 || p->ins <= 0) return MXC_ERR_ARG;
-    if (p->rows > MXC_LINEAR_MAX_ROWS || p->outs > MXC_LINEAR_MAX_DIM || p->ins > MXC_LINEAR_MAX_DIM) return MXC_ERR_SHAPE;
-    Geom g;     // the stored matrices' own limits
-    int rc;
-    if ((rc = geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->rows, p->ins, 1, 1))) return rc;
-    if ((rc = geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->outs, p->ins, 1, 1))) return rc;
-    return geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->rows, p->outs, 1, 1);
-}
-
 // rows, columns and contraction length of a product's output
 static void linear_dims(int op, const mxc_linear& p, int* nrows, int* ncols, int* ncon) {
     *nrows = op == MXC_LINEAR_WGRAD ? p.outs : p.rows;
     *ncols = op == MXC_LINEAR_FWD ? p.outs : p.ins;
     *ncon = op == MXC_LINEAR_FWD ? p.ins : op == MXC_LINEAR_DGRAD ? p.outs : p.rows;
+}
+
+static int linear_check(int op, const mxc_linear* p) {
+    if (p->rows <= 0 || p->outs <= 0 || p->ins <= 0) return MXC_ERR_ARG;
+    if (p->rows > MXC_LINEAR_MAX_ROWS || p->outs > MXC_LINEAR_MAX_DIM || p->ins > MXC_LINEAR_MAX_DIM) return MXC_ERR_SHAPE;
+    int nrows, ncols, ncon;
+    linear_dims(op, *p, &nrows, &ncols, &ncon);
+    if (!linear_fits(op, nrows, ncols)) return MXC_ERR_SHAPE;
+    Geom g;     // the stored matrices' own limits
+    int rc;
+    if ((rc = geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->rows, p->ins, 1, 1))) return rc;
+    if ((rc = geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->outs, p->ins, 1, 1))) return rc;
+    return geom_init(&g, MXC_WEIGHT, MXC_E4M3, p->rows, p->outs, 1, 1);
 }
 
 static bool fn_plain_ok(int fn) { return fn == MXC_FN_NONE || fn == MXC_FN_RELU || fn == MXC_FN_SILU; }
@@ -656,7 +659,7 @@ static int linear_run(int op, const mxc_linear& p, int fa, int fb, const LinMat&
 }
 
 size_t mxconv_linear_workspace_bytes(int op, const mxc_linear* p) {
-    if (!p || op < MXC_LINEAR_FWD || op > MXC_LINEAR_WGRAD || linear_check(p)) return 0;
+    if (!p || op < MXC_LINEAR_FWD || op > MXC_LINEAR_WGRAD || linear_check(op, p)) return 0;
     int nrows, ncols, ncon;
     linear_dims(op, *p, &nrows, &ncols, &ncon);
     return linear_workspace(op, nrows, ncols, ncon);
@@ -667,7 +670,7 @@ int mxconv_linear_fwd(const mxc_linear* p, int fmt, const void* wc, const uint8_
                       int64_t ldy, void* z, int64_t ldz, int dtype, void* workspace, size_t ws_bytes, void* stream) {
     if (!p || !wc || !ws || !xc || !xs || !y) return MXC_ERR_NULL;
     int fw, fx, rc;
-    if ((rc = linear_fmts(fmt, &fw, &fx)) || (rc = linear_check(p))) return rc;
+    if ((rc = linear_fmts(fmt, &fw, &fx)) || (rc = linear_check(MXC_LINEAR_FWD, p))) return rc;
     if (!fn_plain_ok(fn) || (dtype != MXC_F32 && dtype != MXC_BF16)) return MXC_ERR_ARG;
     if (ldy < p->outs || (residual && ldr < p->outs) || (z && ldz < p->outs)) return MXC_ERR_ARG;
     if (z == y || (residual == y && ldr != ldy)) return MXC_ERR_ARG;
@@ -681,7 +684,7 @@ int mxconv_linear_dgrad(const mxc_linear* p, int fmt, const void* wc, const uint
                         void* dx, int64_t ldx, int dtype, void* workspace, size_t ws_bytes, void* stream) {
     if (!p || !wc || !ws || !gc || !gs || !dx) return MXC_ERR_NULL;
     int fw, fg, rc;
-    if ((rc = linear_fmts(fmt, &fw, &fg)) || (rc = linear_check(p))) return rc;
+    if ((rc = linear_fmts(fmt, &fw, &fg)) || (rc = linear_check(MXC_LINEAR_DGRAD, p))) return rc;
     if (!fn_plain_ok(fn) || (dtype != MXC_F32 && dtype != MXC_BF16)) return MXC_ERR_ARG;
     if (fn != MXC_FN_NONE && !z) return MXC_ERR_NULL;
     if (fn == MXC_FN_NONE) z = nullptr;
@@ -696,7 +699,7 @@ int mxconv_linear_wgrad(const mxc_linear* p, int fmt, const void* gc, const uint
                         const uint8_t* xs, float* dw, float* db, void* workspace, size_t ws_bytes, void* stream) {
     if (!p || !gc || !gs || !xc || !xs || !dw) return MXC_ERR_NULL;
     int fg, fx, rc;
-    if ((rc = linear_fmts(fmt, &fg, &fx)) || (rc = linear_check(p))) return rc;
+    if ((rc = linear_fmts(fmt, &fg, &fx)) || (rc = linear_check(MXC_LINEAR_WGRAD, p))) return rc;
     LinEpi e = {dw, nullptr, nullptr, nullptr, p->ins, 0, 0, MXC_FN_NONE, 0, 0, 0, 0};
     return linear_run(LIN_WGRAD, *p, fx, fg, {(const uint8_t*)xc, xs}, {(const uint8_t*)gc, gs}, e, db, workspace,
                       ws_bytes, stream);

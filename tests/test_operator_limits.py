@@ -52,3 +52,65 @@ def test_clip_of_more_than_2_36_elements():
     assert t[1].item() == t[n - 2].item() == c.bfloat16().item()
     bad = sum(int((p != t[1]).sum()) for p in t.split(1 << 32))
     assert bad == len(marks)
+
+
+# ---------------------------------------------------------------- linear layers
+def _linear(op, rows, outs, ins, out=P(0x10001)):
+    """A call whose result is at an odd address, which is refused last."""
+    L, lin, good = mx.lib(), ctypes.byref(mx.MxcLinear(rows, outs, ins)), P(0x10000)
+    ws = (P(0x10000), 1 << 62)
+    if op == 0:
+        return L.mxconv_linear_fwd(lin, 1, good, good, good, good, None, 0, None, 0, out, outs, None, 0, 0, *ws, None)
+    if op == 1:
+        return L.mxconv_linear_dgrad(lin, 1, good, good, good, good, 0, None, 0, None, 0, out, ins, 0, *ws, None)
+    return L.mxconv_linear_wgrad(lin, 1, good, good, good, good, out, None, *ws, None)
+
+
+def test_linear_sizes():
+    """2^30 rows with up to 256 columns of the result, fewer rows with more:
+    2^23 tiles of 128 x 256; a weight gradient 2^22."""
+    top, R = mx.lib().mxconv_linear_workspace_bytes, 1 << 30
+    fine = [(0, R, 256, 64), (0, R, 1, 1), (0, R // 2, 512, 64), (0, 128 * 2048, 1 << 20, 32), (1, R, 64, 256), (1, R // 2, 64, 512),
+            (2, R, 512, 512), (2, 64, 1 << 20, 1 << 17), (2, 64, 1 << 17, 1 << 20)]
+    for op, rows, outs, ins in fine:
+        assert _linear(op, rows, outs, ins) == ALIGN, (op, rows, outs, ins)
+    over = [(0, R, 257, 64), (0, R // 2 + 1, 512, 64), (0, 128 * 2048 + 1, 1 << 20, 32), (1, R, 64, 257), (1, R // 2 + 1, 64, 512),
+            (2, 64, 1 << 20, (1 << 17) + 1), (2, 64, 1 << 20, 1 << 20)]
+    for op, rows, outs, ins in over:
+        assert _linear(op, rows, outs, ins) == SHAPE, (op, rows, outs, ins)
+        assert top(op, ctypes.byref(mx.MxcLinear(rows, outs, ins))) == 0
+
+
+@pytest.mark.gpu
+def test_linear_of_2_30_rows():
+    """FP4 codes as they come under a scale of one: sums of 32 products of at
+    most 36, in quarters, are exact in fp32, so the rows of any 32-row block
+    equal those of the block alone."""
+    if not torch.cuda.is_available() or torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 100 GB of device memory")
+    rows, k = (1 << 30) - 5, 32
+    g = torch.Generator(DEV).manual_seed(1)
+    nb = (rows + 31) // 32
+    codes = torch.randint(0, 256, (nb * 512,), dtype=torch.uint8, device=DEV, generator=g)
+    scales = torch.full((nb,), 127, dtype=torch.uint8, device=DEV)
+    x = mx.MxTensor(codes, scales, mx.WEIGHT, mx.E2M1, (rows, k, 1, 1))
+    wf = torch.randn((k, k), device=DEV, generator=g)
+    blocks = [0, 1 << 22, (1 << 24) - 1, 1 << 24, (1 << 24) + 1, nb - 2, nb - 1]
+    for call in (lambda m: mx.linear(mx.quantize_matrix(wf[:3], mx.E2M1), m, fn=mx.FN_RELU, dtype=torch.bfloat16),
+                 lambda m: mx.linear_dgrad(mx.quantize_matrix(wf[:, :1].contiguous(), mx.E2M1), m, dtype=torch.bfloat16)):
+        y = call(x)
+        assert y.shape[0] == rows
+        for b in blocks:
+            n = min(32, rows - 32 * b)
+            part = mx.MxTensor(codes[512 * b:512 * b + 512].clone(), scales[b:b + 1].clone(), mx.WEIGHT, mx.E2M1, (n, k, 1, 1))
+            assert torch.equal(y[32 * b:32 * b + n], call(part)), b
+        del y
+    # the same codes as the contraction of a weight gradient: integers of fp32 while the sums stay small
+    ones = mx.MxTensor(torch.full((nb * 512,), 0x22, dtype=torch.uint8, device=DEV), scales, mx.WEIGHT, mx.E2M1, (rows, k, 1, 1))
+    few = torch.zeros_like(codes)
+    for b in blocks:
+        few[512 * b] = 0x02                                                  # row 32 b, column 0
+    dw, db = mx.linear_wgrad(mx.MxTensor(few, scales, mx.WEIGHT, mx.E2M1, (rows, k, 1, 1)), ones)
+    want = torch.zeros(k, device=DEV)
+    want[0] = len(blocks)
+    assert torch.equal(db, want) and torch.equal(dw, want[:, None].expand(k, k))
