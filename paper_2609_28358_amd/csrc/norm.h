@@ -43,9 +43,7 @@ struct NormArgs {
     float* p_gate;                     // and dgate itself
     long long rows, gates, gate_rows, run, runs, runs_per_gate, gates_per_run;
     int d;
-    bool nt;                           // results of 4 MiB or more, in whole cache lines: non-temporal stores
-                                       // (fp32 16384 x 1024: forward 52 -> 43, backward 100 -> 76 us; bf16
-                                       // 4096 x 1024 9.4 -> 7.5 and 22 -> 20; rows of 4095 bf16 backward 175 -> 187)
+    bool nt;                           // non-temporal stores of the results (norm.hip, past())
     float scale, eps, inv_d;
 };
 

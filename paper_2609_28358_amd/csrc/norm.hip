@@ -476,13 +476,32 @@ void plan_runs(NormArgs& a) {
 }  // namespace
 
 // Results whose rows begin at cache lines (ld: their row stride).
-static bool lines(const NormArgs& a, bool bf16, const void* p, long long ld) {
+static bool lines(bool bf16, const void* p, long long ld) {
     const int es = bf16 ? 2 : 4;
-    return !p || (a.rows * a.d * es >= (4 << 20) && (uintptr_t)p % 128 == 0 && ld * es % 128 == 0);
+    return !p || ((uintptr_t)p % 128 == 0 && ld * es % 128 == 0);
+}
+// Whether results are stored non-temporally, by the bytes of one.  Measured with
+// other inputs in between, plain -> non-temporal stores, us, and in brackets with
+// the quantization of U, or of dX and dY, behind them:
+//                            forward                       backward
+//   2 MiB (bf16 1024 rows)   6.0 -> 6.0 (9.7 -> 9.6)       13.5 -> 13.6 (20.7 -> 20.7)
+//   4     (bf16 2048)        7.9 -> 7.1 (12.6 -> 12.1)     18.8 -> 17.7 (28.1 -> 27.8)
+//   8     (bf16 4096)        11.9 -> 9.9 (18.3 -> 17.1)    24.8 -> 21.8 (37.9 -> 36.3)
+//   16    (bf16 8192)        18.2 -> 18.4 (29.1 -> 29.5)   33.6 -> 32.7 (54.6 -> 55.5)
+//   32    (bf16 16384)       31.1 -> 31.1 (47.8 -> 51.1)   53.0 -> 52.8 (86.2 -> 93.1)
+//   64    (fp32 16384)       63.2 -> 62.8 (81.0 -> 85.5)   94.8 -> 91.3 (134.9 -> 136.8)
+//   128   (fp32, d 4096)     112 -> 120 (154 -> 155)       188 -> 184 (272 -> 265)
+// (d 1024): from 16 MiB on the last-level cache still holds plain results for
+// what reads them next, until the backward pass's tensors no longer fit it
+// together.  Rows that begin inside cache lines lose by them (backward, bf16 rows
+// of 4095: 175 -> 187).
+static bool past(const NormArgs& a, bool bf16, bool bwd) {
+    const long long mib = (a.rows * a.d * (bf16 ? 2 : 4)) >> 20;
+    return (mib >= 4 && mib < 16) || (bwd && mib >= 128);
 }
 
 int launch_norm_fwd(NormArgs a, bool bf16, hipStream_t s) {
-    a.nt = lines(a, bf16, a.h, a.ldh) && lines(a, bf16, a.u, a.ldu);
+    a.nt = past(a, bf16, false) && lines(bf16, a.h, a.ldh) && lines(bf16, a.u, a.ldu);
     const long long rl = norm_fwd_rows(a.d);
     a.run = std::max<long long>(rl, (a.rows + norm_fwd_runs(a.d) - 1) / norm_fwd_runs(a.d));
     return launch(a, false, bf16, (unsigned)((a.rows + a.run - 1) / a.run), s);
@@ -503,7 +522,7 @@ size_t norm_bwd_workspace(long long rows, int d, long long gates, bool gate, boo
 
 int launch_norm_bwd(NormArgs a, bool bf16, float* dw_pre, float* dw_post, float* dgate, void* ws, hipStream_t s) {
     plan_runs(a);
-    a.nt = lines(a, bf16, a.dx, a.lddx) && lines(a, bf16, a.dy, a.lddy);
+    a.nt = past(a, bf16, true) && lines(bf16, a.dx, a.lddx) && lines(bf16, a.dy, a.lddy);
     const bool one = a.runs == 1;                 // a single workgroup writes the results itself
     float* p = (float*)ws;
     auto take = [&](float* dst) {
