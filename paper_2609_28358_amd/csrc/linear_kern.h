@@ -43,20 +43,32 @@ struct LinOp {
 // The epilogue: out[r][c] for output row r < nrows, column c < ncols.
 //   fwd    z = v + bias[c]; pre[r][c] = z; out = fn(z) + res[r][c]
 //   dgrad  out = v fn'(z[r][c]) + res[r][c]
-// pre doubles as dgrad's z.  nt: the results are 4 MiB or more and their rows
-// begin at cache lines: non-temporal stores, which take less from the loads beside
-// them and from what reads the results next (MXFP4 4096 x 1024 x 1024 with its
-// pre-activation 10.7 -> 9.4 us, and with the quantization of the result behind it
-// 18.0 -> 16.3; 16384 x 300 x 8192 145 -> 122; at 2 MB, 1024 x 1024 x 1024 with the
-// quantization, 9.6 -> 9.8.  Rows that begin elsewhere lose by them, 16384 x 300 x
-// 8191 186 -> 241).
+// pre doubles as dgrad's z.  nt, ntp: out or pre is stored non-temporally, by its
+// bytes and where its rows begin at cache lines (rows that begin elsewhere lose by
+// it, 16384 x 300 x 8191 186 -> 241 us).  Measured with other inputs in between,
+// plain stores -> non-temporal out, us, and in brackets with the quantization of
+// the result behind it; rows x outs x ins, MXFP4 and MXFP8, bf16 results:
+//                                  forward with residual         input gradient
+//    4 MiB, fp4  2048 x 1024 x 1024  7.6 -> 7.4 (12.4 -> 12.7)     6.9 -> 6.8 (11.2 -> 11.3)
+//    8,     fp8  4096 x 1024 x 1024  16.5 -> 16.0 (23.4 -> 23.2)   14.7 -> 13.7 (22.2 -> 21.7)
+//   16,     fp4  8192 x 1024 x 1024  16.1 -> 15.9 (26.3 -> 27.1)   13.7 -> 11.5 (24.5 -> 23.2)
+//   32,     fp4 16384 x 1024 x 1024  28.2 -> 27.7 (44.8 -> 47.2)   21.4 -> 18.5 (38.8 -> 38.4)
+//   32,     fp8  4096 x 4096 x 1024  46.6 -> 45.1 (63.8 -> 66.5)   36.7 -> 34.8 (55.1 -> 57.2)
+//   64,     fp4  8192 x 4096 x 1024  51.4 -> 50.6 (82.9 -> 86.2)   36.8 -> 34.8 (69.4 -> 72.1)
+//  128,     fp8 16384 x 4096 x 1024  159 -> 157 (227 -> 224)       124 -> 122 (191 -> 198)
+// From 32 MiB on the last-level cache still holds a plain result for what reads it
+// next, so out is stored so from 4 to 32 MiB (fp32 weight gradients with an update
+// behind them: 16 MiB, fp8 47.6 -> 46.9; 64 MiB, fp4 76.9 -> 82.9).  The
+// pre-activation, which is read much later, is from 4 MiB on: MXFP4 with SiLU, both
+// results at 8 MiB 11.7 -> 9.5 (18.4 -> 17.2), pre alone at 64 MiB 51.2 -> 49.9
+// (83.5 -> 82.6) and at 128 MiB 98.2 -> 95.7 (171 -> 162).
 struct LinEpi {
     void* out;
     const float* bias;
     const void* res;
     void* pre;
     long long ldo, ldr, ldp;
-    int fn, bf16, nt;
+    int fn, bf16, nt, ntp;
     int nrows, ncols;
 };
 
@@ -238,7 +250,7 @@ __device__ __forceinline__ void lin_finish(const LinEpi& e, int r, int c, float*
     if (OP == LIN_FWD && e.pre) {
 #pragma unroll
         for (int q = 0; q < N; q++) z[q] = v[q] + b[q];
-        lin_store<BF, N>(e.pre, r * e.ldp + c, left, z, e.nt);
+        lin_store<BF, N>(e.pre, r * e.ldp + c, left, z, e.ntp);
     }
 #pragma unroll
     for (int q = 0; q < N; q++) v[q] = lin_value<OP>(FN, v[q], b[q], z[q], s[q]);

@@ -652,9 +652,10 @@ static int linear_run(int op, const mxc_linear& p, int fa, int fb, const LinMat&
         !aligned_to(MXC_F32, colsum) || (need && !aligned16(ws)))
         return MXC_ERR_ALIGN;
     const int es = e.bf16 ? 2 : 4;
-    const bool written = op != LIN_DGRAD && e.pre;            // a second result (the input gradient only reads it)
-    e.nt = (int64_t)e.nrows * e.ncols * es >= (4 << 20) && e.ldo * es % 128 == 0 && (uintptr_t)e.out % 128 == 0 &&
-           (!written || (e.ldp * es % 128 == 0 && (uintptr_t)e.pre % 128 == 0));
+    const int64_t mib = ((int64_t)e.nrows * e.ncols * es) >> 20;
+    auto lines = [es](const void* m, int64_t ld) { return ld * es % 128 == 0 && (uintptr_t)m % 128 == 0; };
+    e.nt = mib >= 4 && mib < 32 && lines(e.out, e.ldo);
+    e.ntp = op == LIN_FWD && e.pre && mib >= 4 && lines(e.pre, e.ldp);
     return launch_linear(op, fa, fb, a, b, ncon, e, colsum, ws, (hipStream_t)stream);
 }
 
@@ -674,7 +675,7 @@ int mxconv_linear_fwd(const mxc_linear* p, int fmt, const void* wc, const uint8_
     if (!fn_plain_ok(fn) || (dtype != MXC_F32 && dtype != MXC_BF16)) return MXC_ERR_ARG;
     if (ldy < p->outs || (residual && ldr < p->outs) || (z && ldz < p->outs)) return MXC_ERR_ARG;
     if (z == y || (residual == y && ldr != ldy)) return MXC_ERR_ARG;
-    LinEpi e = {y, bias, residual, z, ldy, ldr, ldz, fn, dtype == MXC_BF16, 0, 0, 0};
+    LinEpi e = {y, bias, residual, z, ldy, ldr, ldz, fn, dtype == MXC_BF16, 0, 0, 0, 0};
     return linear_run(LIN_FWD, *p, fw, fx, {(const uint8_t*)wc, ws}, {(const uint8_t*)xc, xs}, e, nullptr, workspace,
                       ws_bytes, stream);
 }
@@ -690,7 +691,7 @@ int mxconv_linear_dgrad(const mxc_linear* p, int fmt, const void* wc, const uint
     if (fn == MXC_FN_NONE) z = nullptr;
     if (ldx < p->ins || (residual && ldr < p->ins) || (z && ldz < p->ins)) return MXC_ERR_ARG;
     if ((residual == dx && ldr != ldx) || (z == dx && ldz != ldx)) return MXC_ERR_ARG;
-    LinEpi e = {dx, nullptr, residual, const_cast<void*>(z), ldx, ldr, ldz, fn, dtype == MXC_BF16, 0, 0, 0};
+    LinEpi e = {dx, nullptr, residual, const_cast<void*>(z), ldx, ldr, ldz, fn, dtype == MXC_BF16, 0, 0, 0, 0};
     return linear_run(LIN_DGRAD, *p, fw, fg, {(const uint8_t*)wc, ws}, {(const uint8_t*)gc, gs}, e, nullptr, workspace,
                       ws_bytes, stream);
 }
@@ -700,7 +701,7 @@ int mxconv_linear_wgrad(const mxc_linear* p, int fmt, const void* gc, const uint
     if (!p || !gc || !gs || !xc || !xs || !dw) return MXC_ERR_NULL;
     int fg, fx, rc;
     if ((rc = linear_fmts(fmt, &fg, &fx)) || (rc = linear_check(MXC_LINEAR_WGRAD, p))) return rc;
-    LinEpi e = {dw, nullptr, nullptr, nullptr, p->ins, 0, 0, MXC_FN_NONE, 0, 0, 0, 0};
+    LinEpi e = {dw, nullptr, nullptr, nullptr, p->ins, 0, 0, MXC_FN_NONE, 0, 0, 0, 0, 0};
     return linear_run(LIN_WGRAD, *p, fx, fg, {(const uint8_t*)xc, xs}, {(const uint8_t*)gc, gs}, e, db, workspace,
                       ws_bytes, stream);
 }
