@@ -677,6 +677,9 @@ int mxconv_quantize_sum_sr(int fmt, int n, int c, int h, int w, int nterms, cons
  *             itself (same pointer and stride).
  *   z         NULL, or device `dtype` rows x outs, row stride ldz: receives Z,
  *             rounded; fn is applied to the unrounded Z.
+ * In all three products a result may not share elements with an operand or
+ * another result in any way but those named here (for the input gradient: z or
+ * the residual may be dX itself).
  * Input gradient:  dX = fn'(z) . (dZ W) + residual, rows x ins -- with z the
  * pre-activation whose activation is this layer's X, the dZ of the layer
  * before; with the gradient that reached X past this layer as the residual.
@@ -730,7 +733,8 @@ int mxconv_linear_wgrad(const mxc_linear* lin, int fmt,
  *   gate    NULL (1), or device fp32 [gates][d]: row r has gate r / (rows /
  *           gates); gates divides rows (one gate for all rows: gates = 1);
  *   w_pre   NULL (no U), or device fp32 [d];
- *   h, u    written; h may be x itself (same pointer and stride).
+ *   h, u    written; h may be x itself (same pointer and stride).  Results share
+ *           no elements with operands or each other in any other way.
  * Backward, from the gradients dH of H and dU of U, with H and Y as the
  * forward pass wrote and read them (the statistics are formed again):
  *   t = dU . w_pre, hh = H r(H):  dX = dH + r(H) (t - hh mean(t . hh)),
@@ -774,9 +778,9 @@ int mxconv_norm_bwd(const mxc_norm* nm, const void* dh, int64_t lddh, const void
  * of n >= 0 elements, fp32 or bf16 each, and need no more than their elements'
  * alignment (slices of one buffer).
  *   dst        every tensor's output (its src: in place), or NULL in all of
- *              them: only the norm is formed.  What is written (outputs, norm,
- *              workspace) must not overlap, nor a src, but for outputs that are
- *              their own src: an ARG error.
+ *              them: only the norm is formed.  What is written (outputs and
+ *              the norm beside them, workspace) must not overlap, nor a src, but
+ *              for outputs that are their own src: an ARG error.
  *   max_norm   >= 0 (infinity: a finite norm is never scaled).
  *   norm       NULL, or device fp32 [1], written (0 for no elements).
  *   workspace  device, >= mxconv_grad_clip_workspace_bytes() bytes, 16-byte aligned.

@@ -781,12 +781,13 @@ int mxconv_norm_bwd(const mxc_norm* p, const void* dh, int64_t lddh, const void*
 // ---- gradient clipping
 size_t mxconv_grad_clip_workspace_bytes(void) { return (size_t)CLIP_PARTS * sizeof(double); }
 
-// Whether something that is written -- an output, the norm, the workspace --
-// shares bytes with another written range, or with a source that is not that
-// output itself.  The written ranges are put in order; then a neighbour that
+// Whether something that is written -- an output, the norm beside outputs, the
+// workspace -- shares bytes with another written range, or with a source that is
+// not that output itself.  (Without outputs the norm is written when all else has
+// been read.)  The written ranges are put in order; then a neighbour that
 // begins before the end is an overlap, and a source is looked up by its last
 // byte.  (Addresses that wrap around are not met: they are real allocations'.)
-static int clip_disjoint(int count, const mxc_gtensor* t, const float* norm, const void* ws, size_t ws_bytes) {
+static int clip_disjoint(int count, const mxc_gtensor* t, bool scale, const float* norm, const void* ws, size_t ws_bytes) {
     struct Span {
         uintptr_t begin, end;
     };
@@ -802,7 +803,7 @@ static int clip_disjoint(int count, const mxc_gtensor* t, const float* norm, con
     int n = 0;
     for (int i = 0; i < count; i++)
         if (t[i].n && t[i].dst) w[n++] = span(t[i].dst, bytes(t[i]));
-    if (norm) w[n++] = span(norm, sizeof(float));
+    if (scale && norm) w[n++] = span(norm, sizeof(float));
     w[n++] = span(ws, ws_bytes);
     std::sort(w, w + n, [](const Span& a, const Span& b) { return a.begin < b.begin; });
     for (int i = 1; i < n; i++)
@@ -836,7 +837,7 @@ int mxconv_grad_clip(int count, const mxc_gtensor* t, double max_norm, float* no
     }
     const bool scale = full >= 0 && t[full].dst;
     if (!scale && !norm) return full >= 0 ? MXC_ERR_NULL : MXC_OK;   // nothing to write
-    if (const int rc = clip_disjoint(count, t, norm, workspace, mxconv_grad_clip_workspace_bytes())) return rc;
+    if (const int rc = clip_disjoint(count, t, scale, norm, workspace, mxconv_grad_clip_workspace_bytes())) return rc;
     return launch_grad_clip(count, t, scale, max_norm, norm, workspace, (hipStream_t)stream);
 }
 

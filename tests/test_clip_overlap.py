@@ -44,7 +44,7 @@ def test_overlaps(specs):
 def test_norm_and_workspace():
     assert _call((A, B, 100, F32), norm=A + 4) == ARG
     assert _call((A, B, 100, F32), norm=B + 396) == ARG
-    assert _call((A, 0, 100, F32), norm=A) == ARG
+    assert _call((A, 0, 100, F32), ws=A - 16) == ARG
     assert _call((A, B, 100, F32), norm=WS + 16) == ARG
     assert _call((A, B, 100, F32), ws=B + 16) == ARG
     assert _call((A, A, 100, F32), ws=A - 16) == ARG
@@ -67,6 +67,14 @@ def test_refused_in_python(gpu):
         with pytest.raises(mx.MxconvError):
             call()
     assert (a == 1).all() and (b == 2).all() and (flat == 3).all()
+
+
+@pytest.mark.gpu
+def test_norm_alone_may_lie_in_a_tensor(gpu):
+    """Without outputs the norm is written when all has been read."""
+    flat = torch.ones(10000, device=gpu)
+    assert float(mx.grad_norm([flat], norm_out=flat[77])) == 100.0
+    assert flat[77] == 100.0 and int((flat != 1).sum()) == 1
 
 
 @pytest.mark.gpu
