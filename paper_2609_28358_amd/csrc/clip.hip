@@ -10,8 +10,11 @@
 // its chunk by counting, lane by lane, the tensors that begin no later.  Each workgroup of the norm
 // leaves one partial sum; every workgroup of the scaling adds all of them, in
 // the same order, so the result does not depend on timing and there is no
-// third launch.  300 bf16 tensors of 1.15 GB together: norm 188 us (6.1 TB/s),
-// scaling 492 (4.7 TB/s); 60 fp32 ones of 19 MB 6.9 and 10.5 us.
+// third launch.  Other inputs in between, each pass waited for: 300 bf16 tensors of
+// 1.15 GB together norm 196 us (5.9 TB/s; a copy of 2 GiB reaches 5.0), scaling 494
+// (4.7 TB/s); 60 fp32 ones of 19 MB 8.0 and 11.1 us.  The launches share CLIP_PARTS
+// partial sums, and with them the workgroups: from the second launch on each has
+// fewer (2000 tensors 409 a launch, 65536 13).
 #include "mx_internal.h"
 #include "clip.h"
 
@@ -131,8 +134,11 @@ __global__ __launch_bounds__(CT) void clip_scale_kernel(const ClipArgs a, const 
         const long long b0 = (long long)(k - a.first[t]) * a.chunk;
         const uint8_t* p = (const uint8_t*)a.src[t] + b0;
         uint8_t* d = (uint8_t*)a.dst[t] + b0;
-        // non-temporal where the vectors are aligned (300 bf16 tensors, 600 MB: both
-        // launches 343 -> 316 us)
+        // non-temporal where the vectors are aligned: 60 tensors, other inputs in
+        // between, both launches, plain stores -> these, and in brackets with an update
+        // that reads the results behind them, us: fp32 2 MB 8.6 -> 8.7 (15.0 -> 15.1), 8 MB
+        // 13.8 -> 12.6 (26.3 -> 25.4), 40 MB 31.6 -> 28.2 (62.2 -> 59.5), 160 MB 103 -> 89
+        // (225 -> 221), 640 MB 376 -> 357 (808 -> 800); bf16 alike; in place no difference
         const bool nt = ((uintptr_t)d & 15) == 0;
         const int len = (int)min((long long)a.chunk, bytes - b0);
         vectors(len, [&](int o, auto num) {

@@ -18,12 +18,14 @@
 // a lane's accumulator holds four consecutive output columns of one output
 // row and the epilogue moves vectors.
 //
-// What bounds it: large MXFP8 products the matrix units and their power (16384 x
-// 4096 x 4096 437 us, 1.26 PFLOP/s; loops of the MFMAs alone reach 1.4); large
-// MXFP4 ones the bytes of their results (4096 x 4096 x 1024 with SiLU and the
-// pre-activation kept 24 us, 71 MB at 3.0 TB/s);
-// few rows the weights' bytes (24 x 8192 x 8192 MXFP8 13.9 us, 5.0 TB/s); small
-// ones a chain of stages behind the launch (1 x 4096 x 1024 MXFP4 5.6 us).
+// What bounds it (a pass among others on other inputs): large MXFP8 products the
+// matrix units and their power (16384 x 4096 x 4096 436 to 446 us on different
+// cards, 1.23 to 1.26 PFLOP/s, the matrix cores busy 48% of the cycles at 2.4 GHz; loops of
+// the MFMAs alone reach 1.4 PFLOP/s); large MXFP4 ones the bytes of their results,
+// stored behind the products (4096 x 4096 x 1024 with SiLU and the pre-activation
+// kept 24.5 us, 71 MB at 2.9 TB/s, the matrix cores busy 13%); few rows the weights'
+// bytes (24 x 8192 x 8192 MXFP8 13.7 us, 5.0 TB/s); small ones a chain of stages
+// behind the launch (1 x 4096 x 1024 MXFP4 4.9 us of the GPU).
 #pragma once
 #include <atomic>
 

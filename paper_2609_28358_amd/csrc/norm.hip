@@ -11,8 +11,14 @@
 // What bounds both is memory: a row is read once and held in registers (8
 // values of each tensor a thread, 16 of the longest rows), with two sums over the
 // row forward (Y's square, then H's) and two rounds of sums backward (the second
-// one needs dX).  bf16: forward 8192 x 4096 45 us (6.0 TB/s), backward 16384 x
-// 1024 40 us (5.0 TB/s) and 6 for the join; a copy of 2 GiB reaches 5.0 TB/s.
+// one needs dX).  bf16, other inputs in between: forward 8192 x 4096 57 us a pass
+// among others (4.7 TB/s; 49 waited for alone, when the last results are still on
+// their way out of the caches), backward 16384 x 1024 53 (3.8 TB/s; 43 alone and 6
+// for the join); a copy of 2 GiB reaches 5.0 TB/s.
+// Four waves a SIMD leave 128 registers, and some kernels spill a few: 2 to 4 in
+// the backward pass of rows of 2049 to 4096, 8 in the bf16 forward of longer ones,
+// and 6 to 18 (up to 76 bytes) where workgroups take whole gates, of bf16 rows up
+// to 4096 and fp32 rows of 1025 to 4096.
 // A workgroup takes a run of consecutive rows, so the weights and the gate are
 // loaded once a run; backward, its column sums stay in registers until the
 // run's end and are added over the workgroups by a second kernel, in order.
