@@ -12,9 +12,9 @@
 // the same order, so the result does not depend on timing and there is no
 // third launch.  Other inputs in between, each pass waited for: 300 bf16 tensors of
 // 1.15 GB together norm 196 us (5.9 TB/s; a copy of 2 GiB reaches 5.0), scaling 494
-// (4.7 TB/s); 60 fp32 ones of 19 MB 8.0 and 11.1 us.  The launches share CLIP_PARTS
-// partial sums, and with them the workgroups: from the second launch on each has
-// fewer (2000 tensors 409 a launch, 65536 13).
+// (4.7 TB/s); 60 fp32 ones of 19 MB 8.0 and 11.1 us.  All launches
+// together have CLIP_PARTS workgroups, one a partial sum: the more tensors, the
+// fewer workgroups a launch (2000 tensors 409, 65536 13).
 #include "mx_internal.h"
 #include "clip.h"
 
